@@ -1,0 +1,131 @@
+// dense.h -- products of dense matrices with their epilogues, and the small
+// kernels around them: the launchers behind include/singa_mi_dense.h.  Like
+// internal.h, everything here takes arguments that the ABI layer has checked.
+#pragma once
+
+#include "internal.h"
+
+namespace singa {
+
+enum Act { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
+
+// What a product does with its sum over k, element (row, col) of M x N.
+//   EPI_OUT     v = alpha sum + bias[col]; z = v (kept when z is given);
+//               y = act(v) + res, or y += that (add, fp32 outputs), zeroed in
+//               rows without a valid label (labels given)
+//   EPI_LSE     the maximum and the sum of exponentials of v = sum + bias[col]
+//               over each STAT_COLS columns, and v at the row's label: the
+//               logits themselves are not stored
+//   EPI_DLOGITS exp(v - lse[row]) - [col is the row's label] in rows with a
+//               valid label, else 0, stored in the product's type (and, with
+//               more, what that rounding left).  The factor scale / count of the
+//               loss is left to the products that take these (alpha), so that
+//               a label's entry, nearly -1, is stored nearly exactly: with the
+//               factor in it, its rounding was the same for every row and put
+//               0.3 % on all of dx.
+enum Epi { EPI_OUT = 0, EPI_LSE = 1, EPI_DLOGITS = 2 };
+
+constexpr int STAT_COLS = 64;
+
+struct Epilogue {
+  const float* alpha = nullptr;  // one value
+  const float* bias = nullptr;  // [N]
+  int act = ACT_NONE;
+  const void* res = nullptr;  // T [M][N]
+  void* z = nullptr;          // T [M][N]
+  void* y = nullptr;          // T or fp32 [M][ldy]
+  long ldy = 0;
+  int out_f32 = 0, add = 0;
+  // loss: labels counted from column col0 of this product
+  const int32_t* labels = nullptr;
+  int classes = 0;  // a label is valid in [0, classes)
+  int col0 = 0;
+  float2* stats = nullptr;  // [M][nstat] (maximum, sum), column group stat0 + ...
+  int nstat = 0, stat0 = 0;
+  float* zlab = nullptr;       // [M]
+  const float* lse = nullptr;  // [M]
+  bf16_t* more = nullptr;  // the further terms (see TERMS), one behind the other
+  int rows_padded = 0;  // dlogits rows from M up to here are zeroed (a sum over two halves reads them)
+  float* colsum = nullptr;  // [row groups][N]: sums of the dlogits over COLSUM_ROWS rows
+};
+
+constexpr int COLSUM_ROWS = 64;
+
+// An operand: logical rows x K.  kc: stored row by row (K contiguous, ld
+// elements from row to row); otherwise stored k by k (rows contiguous, ld
+// elements from k to k).  The stored rows start at 16-byte boundaries, and
+// what lies between their end and the next such boundary is zero.
+struct Operand {
+  const void* p;
+  long ld;
+  bool kc;
+};
+
+// y (M x N) = epilogue(A B^T), A: M x K, B: N x K.
+struct Product {
+  int dt = BF16;
+  int M = 0, N = 0, K = 0;
+  Operand a{}, b{};
+  // a k index from `wrap` on continues in A and starts again in B, and so from
+  // 2 wrap on: A's terms one behind the other, each with the same B.  A
+  // multiple of K_TILE elements; 0: one term.  K counts all terms.
+  int wrap = 0;
+  int kb = 0;  // k rows that B has (0: K)
+  int epi = EPI_OUT;
+  Epilogue e;
+  const char* name = "";
+  double flops = 0;
+};
+
+// An fp32 gradient of bf16 weights takes a computed dz (fp32) in this many
+// bf16 terms, each the rounding of what the ones before left: 3 x 8 bits of
+// significand hold all of fp32's 24.  (Two, an error of 2^-18 at most, put
+// 1.2e-6 on dw where the fp32 sums alone leave 0.3e-6; one 1.6e-3.)
+constexpr int TERMS = 3;
+
+constexpr int K_TILE = 64;  // a multiple of every kernel's K-tile
+
+// Workspace for the partial sums of a product whose tiles cannot fill the GPU.
+size_t product_partial_bytes(int dt, int M, int N, int K, int epi);
+hipError_t launch_product(const Product& p, float* partial, hipStream_t st);
+
+// The same product for few rows (M <= SKINNY_ROWS), A and B both K contiguous
+// with ld = K, any alignment: a pass over B.  EPI_OUT and EPI_LSE (STAT_COLS
+// of SKINNY_COLS columns).
+constexpr int SKINNY_ROWS = 64, SKINNY_COLS = 16;
+hipError_t launch_skinny(const Product& p, hipStream_t st);
+
+// Zeros, by a kernel (a captured memset node is not replayed reliably).
+hipError_t launch_zero(void* p, size_t bytes, hipStream_t st);
+// out [rows][ldo] = in [rows][cols], zero from cols to ldo; rows without a
+// valid label (labels given) become zero.
+hipError_t launch_pack(int dt, const void* in, void* out, long rows, int cols, long ldo, const int32_t* labels,
+                       int classes, hipStream_t st);
+// dz = dy act'(z) as T [rows_padded][ldz] (zero past rows and cols), more (may
+// be null) its further terms, colsum [ceil(rows / COLSUM_ROWS)][cols]
+// (may be null) the sums of the unrounded dz; dz may be null.
+hipError_t launch_dact(int dt, int act, const void* dy, const void* z, void* dz, void* more, float* colsum, long rows,
+                       long rows_padded, int cols, long ldz, hipStream_t st);
+// out[c] (+)= alpha (null: 1) times the sum of colsum[0 .. groups - 1][c] (in order)
+hipError_t launch_colsum(const float* colsum, float* out, long groups, int cols, int add, const float* alpha,
+                         hipStream_t st);
+// out (T [rows][cols]) = in (fp32 [rows][cols]), zero in rows without a valid label
+hipError_t launch_round_rows(int dt, const float* in, void* out, long rows, int cols, const int32_t* labels,
+                             int classes, hipStream_t st);
+// stats [rows][nstat], zlab -> lse[row], loss[1 + row]
+hipError_t launch_lse(const float2* stats, int nstat, const float* zlab, const int32_t* labels, int classes, long rows,
+                      float* lse, float* loss, hipStream_t st);
+// loss[0] = mean of loss[1 ..] over the counted rows, unit = scale / count (0 when none; may be null)
+hipError_t launch_loss_mean(const int32_t* labels, int classes, long rows, float* loss, float* unit, float scale,
+                            hipStream_t st);
+// Rows of kept logits z (fp32 [rows][ldz], the bias included): loss[1 + row]
+// and, unless null, dlogits dz as EPI_DLOGITS makes them (T [rows_padded][ldd],
+// zero past rows and classes), their further terms, and their unrounded values dzf (fp32
+// [rows][ldz], may be z).
+hipError_t launch_loss_rows(int dt, const float* z, long ldz, const int32_t* labels, long rows, long rows_padded,
+                            int classes, float* loss, void* dz, void* more, long ldd, float* dzf,
+                            hipStream_t st);
+// colsum [groups][cols] of dzf [rows][ld] over COLSUM_ROWS rows each
+hipError_t launch_colsum_rows(const float* dzf, long ld, float* colsum, long rows, int cols, hipStream_t st);
+
+}  // namespace singa

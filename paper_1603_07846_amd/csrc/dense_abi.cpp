@@ -1,0 +1,540 @@
+// dense_abi.cpp -- the C entry points declared in include/singa_mi_dense.h:
+// argument checks, workspace carving and the order of the kernels.  Nothing is
+// enqueued unless every check passes.
+#include "singa_mi_dense.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <climits>
+#include <cmath>
+
+#include "dense.h"
+#include "gradnorm.h"
+
+using namespace singa;
+
+namespace {
+
+inline int status(hipError_t e) { return e == hipSuccess ? SINGA_OK : SINGA_ERR_HIP; }
+inline bool aligned_to(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
+inline long up(long v, long a) { return (v + a - 1) / a * a; }
+inline int vec(int dt) { return dt == BF16 ? 8 : 4; }
+bool dtype_ok(int dt) { return dt == SINGA_F32 || dt == SINGA_BF16; }
+
+constexpr int kMaxFeatures = 1 << 20;  // a row stays below 2^23 bytes, so 256 of them have 32-bit offsets
+
+constexpr int kMaxRows = 1 << 28;
+
+// Hands out 256-byte aligned parts of a workspace (or, from NULL, counts them;
+// the first 256 bytes make up for a base that is only 16-byte aligned).
+struct Carver {
+  char* base;
+  size_t used = 0;
+  explicit Carver(void* p) : base((char*)(((uintptr_t)p + 255) & ~(uintptr_t)255)) {}
+  void* take(size_t bytes) {
+    void* p = base + used;
+    used += (bytes + 255) & ~(size_t)255;
+    return bytes ? p : nullptr;
+  }
+  template <typename T> T* take(size_t n) { return (T*)take(n * sizeof(T)); }
+  size_t bytes() const { return used ? used + 256 : 0; }
+};
+
+int check_ws(const void* ws, size_t have, size_t need) {
+  if (!need) return SINGA_OK;
+  if (!ws || have < need) return SINGA_ERR_WORKSPACE;
+  return aligned_to(ws, 16) ? SINGA_OK : SINGA_ERR_ALIGN;
+}
+
+int shape(int rows, int in, int out) {
+  if (rows < 0 || in < 1 || out < 1) return SINGA_ERR_SHAPE;
+  if (in > kMaxFeatures || out > kMaxFeatures || rows > kMaxRows) return SINGA_ERR_UNSUPPORTED;
+  return SINGA_OK;
+}
+
+// An operand's row length in a form that the tiles take.
+struct Packed {
+  long ld;
+  bool copy;
+};
+Packed packed(int dt, int cols) {
+  const long ld = up(cols, vec(dt));
+  return {ld, ld != cols};
+}
+
+// ---------------------------------------------------------------- forward
+struct FwdWs {
+  Packed k;
+  void *xp, *wp;
+  float* partial;
+};
+
+size_t carve_fwd(int dt, int rows, int in, int out, void* ws, FwdWs* o) {
+  Carver c(ws);
+  if (rows == 0 || rows <= SKINNY_ROWS) {
+    *o = FwdWs{};
+    return 0;
+  }
+  const size_t es = dt_size(dt);
+  o->k = packed(dt, in);
+  o->xp = c.take(o->k.copy ? (size_t)rows * o->k.ld * es : 0);
+  o->wp = c.take(o->k.copy ? (size_t)out * o->k.ld * es : 0);
+  o->partial = (float*)c.take(product_partial_bytes(dt, rows, out, in, EPI_OUT));
+  return c.bytes();
+}
+
+// ---------------------------------------------------------------- backward
+struct BwdWs {
+  Packed k;
+  long ldz, rows_padded;
+  bool own_dz, split;  // dz in the workspace; in TERMS terms
+  void *dz, *more, *xp, *wp;
+  float *colsum, *partial;
+};
+
+size_t carve_bwd(int dt, int rows, int in, int out, int act, int dw_dt, void* ws, BwdWs* o) {
+  Carver c(ws);
+  *o = BwdWs{};
+  if (rows == 0) return 0;
+  const size_t es = dt_size(dt);
+  o->k = packed(dt, in);
+  const Packed n = packed(dt, out);
+  o->split = dt == BF16 && dw_dt == F32 && (act == ACT_GELU || act == ACT_SILU);
+  o->own_dz = act != ACT_NONE || n.copy;
+  o->ldz = o->own_dz ? up(out, 8) : out;
+  o->rows_padded = o->split ? up(rows, K_TILE) : rows;
+  const size_t half = (size_t)o->rows_padded * o->ldz;
+  o->dz = c.take(o->own_dz ? half * (o->split ? TERMS : 1) * es : 0);
+  o->more = o->split ? (char*)o->dz + half * es : nullptr;
+  o->xp = c.take(o->k.copy ? (size_t)rows * o->k.ld * es : 0);
+  o->wp = c.take(o->k.copy ? (size_t)out * o->k.ld * es : 0);
+  o->colsum = c.take<float>(up(rows, COLSUM_ROWS) / COLSUM_ROWS * (size_t)out);
+  o->partial = (float*)c.take(std::max(product_partial_bytes(dt, rows, in, out, EPI_OUT),
+                                       product_partial_bytes(dt, out, in, (int)(o->rows_padded * (o->split ? TERMS : 1)), EPI_OUT)));
+  return c.bytes();
+}
+
+// ------------------------------------------------------------------- loss
+constexpr size_t kKeep = 64u << 20;    // logits of up to this many bytes are kept
+constexpr size_t kPiece = 256u << 20;  // dlogits of a piece of the classes
+
+struct LossWs {
+  Packed k;
+  bool keep, skinny, split, one;  // logits kept; few rows; dlogits in TERMS terms; one piece
+  long ldd, rows_padded, piece;   // dlogits: row length, rows; classes per piece
+  int nstat;
+  long ldl;  // row length of kept logits
+  void *dz, *more, *xc, *xp, *wp;
+  float *unit, *lse, *zlab, *logits, *dxf, *colsum, *partial;
+  float2* stats;
+};
+
+size_t carve_loss(int dt, int rows, int in, int classes, bool grad, int dw_dt, void* ws, LossWs* o) {
+  Carver c(ws);
+  *o = LossWs{};
+  if (rows == 0) return 0;
+  const size_t es = dt_size(dt);
+  o->k = packed(dt, in);
+  o->skinny = rows <= SKINNY_ROWS;
+  o->ldl = up(classes, 8);
+  o->keep = (!o->skinny || grad) && (size_t)rows * o->ldl * 4 <= kKeep;
+  o->split = grad && dt == BF16 && dw_dt == F32;
+  o->rows_padded = o->split ? up(rows, K_TILE) : rows;
+  // copies for the tiles
+  const bool tiles = !o->skinny || grad;
+  o->wp = c.take(tiles && o->k.copy ? (size_t)classes * o->k.ld * es : 0);
+  o->xp = c.take(tiles && o->k.copy ? (size_t)rows * o->k.ld * es : 0);
+  size_t partial = 0;
+  if (o->keep) {
+    o->logits = c.take<float>((size_t)rows * o->ldl);
+    if (!o->skinny) partial = product_partial_bytes(dt, rows, classes, in, EPI_OUT);
+  } else {
+    o->nstat = (classes + (o->skinny ? SKINNY_COLS : STAT_COLS) - 1) / (o->skinny ? SKINNY_COLS : STAT_COLS);
+    o->stats = c.take<float2>((size_t)rows * o->nstat);
+    o->zlab = c.take<float>(rows);
+    o->lse = c.take<float>(rows);
+  }
+  if (grad) {
+    o->unit = c.take<float>(1);
+    // whole tiles of classes per piece
+    long piece = (long)(kPiece / es) / o->rows_padded / 256 * 256;
+    if (piece < 256) piece = 256;
+    o->one = o->keep || piece >= classes;
+    o->piece = o->one ? classes : piece;
+    o->ldd = up(o->piece, 8);
+    const size_t half = (size_t)o->rows_padded * o->ldd;
+    o->dz = c.take(half * es * (o->split ? TERMS : 1));
+    o->more = o->split ? (char*)o->dz + half * es : nullptr;
+    o->xc = c.take((size_t)rows * o->k.ld * es);
+    o->dxf = o->one ? nullptr : c.take<float>((size_t)rows * in);
+    o->colsum = c.take<float>(up(rows, COLSUM_ROWS) / COLSUM_ROWS * (size_t)o->piece);
+    const int kw = (int)(o->rows_padded * (o->split ? TERMS : 1));
+    // the last piece is shorter, and may be cut otherwise
+    const int last = (int)(classes - (classes - 1) / o->piece * o->piece);
+    for (int n : {(int)o->piece, last})
+      partial = std::max({partial, product_partial_bytes(dt, rows, in, n, EPI_OUT), product_partial_bytes(dt, n, in, kw, EPI_OUT)});
+  }
+  o->partial = (float*)c.take(partial);
+  return c.bytes();
+}
+
+Operand op(const void* p, long ld, bool kc) { return Operand{p, ld, kc}; }
+
+}  // namespace
+
+extern "C" {
+
+int singa_linear_fwd_workspace_bytes(singa_dtype dtype, int rows, int in, int out, size_t* bytes) {
+  if (!bytes) return SINGA_ERR_NULL;
+  if (!dtype_ok(dtype)) return SINGA_ERR_UNSUPPORTED;
+  const int rc = shape(rows, in, out);
+  if (rc != SINGA_OK) return rc;
+  FwdWs o;
+  *bytes = carve_fwd(dtype, rows, in, out, nullptr, &o);
+  return SINGA_OK;
+}
+
+int singa_linear_fwd(singa_dtype dtype, int rows, int in, int out, const void* x, const void* w, const float* bias,
+                     singa_act act, const void* residual, void* z, void* y, void* ws, size_t ws_bytes,
+                     singa_stream stream) {
+  if (!dtype_ok(dtype) || act < SINGA_ACT_NONE || act > SINGA_ACT_SILU) return SINGA_ERR_UNSUPPORTED;
+  int rc = shape(rows, in, out);
+  if (rc != SINGA_OK) return rc;
+  if (rows == 0) return SINGA_OK;
+  if (!x || !w || !y) return SINGA_ERR_NULL;
+  if (!aligned_to(x, 16) || !aligned_to(w, 16) || !aligned_to(y, 16) || !aligned_to(z, 16) || !aligned_to(residual, 16) ||
+      !aligned_to(bias, 4))
+    return SINGA_ERR_ALIGN;
+  FwdWs o;
+  rc = check_ws(ws, ws_bytes, carve_fwd(dtype, rows, in, out, nullptr, &o));
+  if (rc != SINGA_OK) return rc;
+  carve_fwd(dtype, rows, in, out, ws, &o);
+  hipStream_t st = (hipStream_t)stream;
+  Product p;
+  p.dt = dtype;
+  p.M = rows;
+  p.N = out;
+  p.K = in;
+  p.flops = 2.0 * rows * in * out;
+  p.e.bias = bias;
+  p.e.act = act;
+  p.e.res = residual;
+  p.e.z = z;
+  p.e.y = y;
+  if (rows <= SKINNY_ROWS) {
+    p.name = "skinny_kernel";
+    p.a = op(x, in, true);
+    p.b = op(w, in, true);
+    return status(launch_skinny(p, st));
+  }
+  hipError_t e = hipSuccess;
+  if (o.k.copy) {
+    e = launch_pack(dtype, x, o.xp, rows, in, o.k.ld, nullptr, 0, st);
+    if (e == hipSuccess) e = launch_pack(dtype, w, o.wp, out, in, o.k.ld, nullptr, 0, st);
+    x = o.xp;
+    w = o.wp;
+  }
+  if (e != hipSuccess) return SINGA_ERR_HIP;
+  p.name = "product_kernel<fwd>";
+  p.a = op(x, o.k.ld, true);
+  p.b = op(w, o.k.ld, true);
+  return status(launch_product(p, o.partial, st));
+}
+
+int singa_linear_bwd_workspace_bytes(singa_dtype dtype, int rows, int in, int out, singa_act act, singa_dtype dw_dtype,
+                                     size_t* bytes) {
+  if (!bytes) return SINGA_ERR_NULL;
+  if (!dtype_ok(dtype) || !dtype_ok(dw_dtype) || act < SINGA_ACT_NONE || act > SINGA_ACT_SILU) return SINGA_ERR_UNSUPPORTED;
+  if (dw_dtype == SINGA_BF16 && dtype != SINGA_BF16) return SINGA_ERR_UNSUPPORTED;
+  const int rc = shape(rows, in, out);
+  if (rc != SINGA_OK) return rc;
+  BwdWs o;
+  *bytes = carve_bwd(dtype, rows, in, out, act, dw_dtype, nullptr, &o);
+  return SINGA_OK;
+}
+
+int singa_linear_bwd(singa_dtype dtype, int rows, int in, int out, const void* x, const void* w, const void* z, singa_act act,
+                     const void* dy, const void* dx_residual, void* dx, void* dw, singa_dtype dw_dtype, float* db,
+                     int accumulate, void* ws, size_t ws_bytes, singa_stream stream) {
+  size_t need = 0;
+  int rc = singa_linear_bwd_workspace_bytes(dtype, rows, in, out, act, dw_dtype, &need);
+  if (rc != SINGA_OK) return rc;
+  if (dw && dw_dtype == SINGA_BF16 && accumulate) return SINGA_ERR_UNSUPPORTED;
+  if (!dx && !dw && !db) return SINGA_ERR_NULL;
+  if (rows && (!dy || (dw && !x) || (dx && !w) || (act != SINGA_ACT_NONE && !z))) return SINGA_ERR_NULL;
+  if (!aligned_to(x, 16) || !aligned_to(w, 16) || !aligned_to(z, 16) || !aligned_to(dy, 16) || !aligned_to(dx_residual, 16) ||
+      !aligned_to(dx, 16) || !aligned_to(dw, 16) || !aligned_to(db, 4))
+    return SINGA_ERR_ALIGN;
+  rc = check_ws(ws, ws_bytes, need);
+  if (rc != SINGA_OK) return rc;
+  hipStream_t st = (hipStream_t)stream;
+  hipError_t e = hipSuccess;
+  if (rows == 0) {
+    if (accumulate) return SINGA_OK;
+    if (dw) e = launch_zero(dw, (size_t)out * in * dt_size(dw_dtype), st);
+    if (e == hipSuccess && db) e = launch_zero(db, (size_t)out * 4, st);
+    return status(e);
+  }
+  BwdWs o;
+  carve_bwd(dtype, rows, in, out, act, dw_dtype, ws, &o);
+  const bool split = o.split && dw;
+  if (o.own_dz || db)
+    e = launch_dact(dtype, act, dy, z, o.own_dz ? o.dz : nullptr, split ? o.more : nullptr, db ? o.colsum : nullptr, rows,
+                    o.rows_padded, out, o.ldz, st);
+  if (e == hipSuccess && db)
+    e = launch_colsum(o.colsum, db, up(rows, COLSUM_ROWS) / COLSUM_ROWS, out, accumulate, nullptr, st);
+  const void* dz = o.own_dz ? o.dz : dy;
+  if (o.k.copy && dx && e == hipSuccess) {
+    e = launch_pack(dtype, w, o.wp, out, in, o.k.ld, nullptr, 0, st);
+    w = o.wp;
+  }
+  if (o.k.copy && dw && e == hipSuccess) {
+    e = launch_pack(dtype, x, o.xp, rows, in, o.k.ld, nullptr, 0, st);
+    x = o.xp;
+  }
+  Product p;
+  p.dt = dtype;
+  p.flops = 2.0 * rows * in * out;
+  if (dx && e == hipSuccess) {
+    p.name = "product_kernel<bwd_data>";
+    p.M = rows;
+    p.N = in;
+    p.K = out;
+    p.a = op(dz, o.ldz, true);
+    p.b = op(w, o.k.ld, false);
+    p.e.res = dx_residual;
+    p.e.y = dx;
+    e = launch_product(p, o.partial, st);
+  }
+  if (dw && e == hipSuccess) {
+    p.name = "product_kernel<bwd_weights>";
+    p.M = out;
+    p.N = in;
+    p.K = split ? (int)(TERMS * o.rows_padded) : rows;
+    p.wrap = split ? (int)o.rows_padded : 0;
+    p.kb = rows;
+    p.a = op(dz, o.ldz, false);
+    p.b = op(x, o.k.ld, false);
+    p.e = Epilogue{};
+    p.e.y = dw;
+    p.e.out_f32 = dw_dtype == SINGA_F32;
+    p.e.add = accumulate != 0;
+    e = launch_product(p, o.partial, st);
+  }
+  return status(e);
+}
+
+int singa_linear_softmax_ce_workspace_bytes(singa_dtype dtype, int rows, int in, int classes, int gradients,
+                                            singa_dtype dw_dtype, size_t* bytes) {
+  if (!bytes) return SINGA_ERR_NULL;
+  if (!dtype_ok(dtype) || !dtype_ok(dw_dtype)) return SINGA_ERR_UNSUPPORTED;
+  if (dw_dtype == SINGA_BF16 && dtype != SINGA_BF16) return SINGA_ERR_UNSUPPORTED;
+  const int rc = shape(rows, in, classes);
+  if (rc != SINGA_OK) return rc;
+  LossWs o;
+  *bytes = carve_loss(dtype, rows, in, classes, gradients != 0, dw_dtype, nullptr, &o);
+  return SINGA_OK;
+}
+
+int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, const void* x, const void* w, const float* bias,
+                            const int32_t* labels, float scale, float* loss, void* dx, void* dw, singa_dtype dw_dtype,
+                            float* db, int accumulate, void* ws, size_t ws_bytes, singa_stream stream) {
+  const bool grad = dx || dw || db;
+  size_t need = 0;
+  int rc = singa_linear_softmax_ce_workspace_bytes(dtype, rows, in, classes, grad, dw_dtype, &need);
+  if (rc != SINGA_OK) return rc;
+  if (dw && dw_dtype == SINGA_BF16 && accumulate) return SINGA_ERR_UNSUPPORTED;
+  if (!loss || !w || (rows && (!x || !labels))) return SINGA_ERR_NULL;
+  if (!aligned_to(x, 16) || !aligned_to(w, 16) || !aligned_to(dx, 16) || !aligned_to(dw, 16) || !aligned_to(bias, 4) ||
+      !aligned_to(labels, 4) || !aligned_to(loss, 4) || !aligned_to(db, 4))
+    return SINGA_ERR_ALIGN;
+  rc = check_ws(ws, ws_bytes, need);
+  if (rc != SINGA_OK) return rc;
+  hipStream_t st = (hipStream_t)stream;
+  hipError_t e = hipSuccess;
+  if (rows == 0) {
+    e = launch_zero(loss, 4, st);
+    if (e == hipSuccess && dw && !accumulate) e = launch_zero(dw, (size_t)classes * in * dt_size(dw_dtype), st);
+    if (e == hipSuccess && db && !accumulate) e = launch_zero(db, (size_t)classes * 4, st);
+    return status(e);
+  }
+  LossWs o;
+  carve_loss(dtype, rows, in, classes, grad, dw_dtype, ws, &o);
+  const void *xt = x, *wt = w;  // as the tiles take them
+  if (o.wp) {
+    e = launch_pack(dtype, w, o.wp, classes, in, o.k.ld, nullptr, 0, st);
+    wt = o.wp;
+  }
+  if (o.xp && e == hipSuccess) {
+    e = launch_pack(dtype, x, o.xp, rows, in, o.k.ld, nullptr, 0, st);
+    xt = o.xp;
+  }
+  Product p;
+  p.dt = dtype;
+  p.M = rows;
+  p.N = classes;
+  p.K = in;
+  p.flops = 2.0 * rows * in * classes;
+  p.e.bias = bias;
+  p.e.labels = labels;
+  p.e.classes = classes;
+  if (o.skinny) {
+    p.a = op(x, in, true);
+    p.b = op(w, in, true);
+  } else {
+    p.a = op(xt, o.k.ld, true);
+    p.b = op(wt, o.k.ld, true);
+  }
+  const bool split = o.split && dw;
+  void* more = split ? o.more : nullptr;
+  const long groups = up(rows, COLSUM_ROWS) / COLSUM_ROWS;
+  if (o.keep) {
+    // the logits, then their rows
+    p.e.labels = nullptr;
+    p.e.y = o.logits;
+    p.e.ldy = o.ldl;
+    p.e.out_f32 = 1;
+    if (e == hipSuccess) {
+      p.name = o.skinny ? "skinny_kernel" : "product_kernel<logits>";
+      e = o.skinny ? launch_skinny(p, st) : launch_product(p, o.partial, st);
+    }
+    if (e == hipSuccess)
+      e = launch_loss_rows(dtype, o.logits, o.ldl, labels, rows, o.rows_padded, classes, loss, grad ? o.dz : nullptr, more,
+                           o.ldd, db ? o.logits : nullptr, st);
+  } else {
+    p.epi = EPI_LSE;
+    p.e.stats = o.stats;
+    p.e.nstat = o.nstat;
+    p.e.zlab = o.zlab;
+    if (e == hipSuccess) {
+      p.name = o.skinny ? "skinny_kernel" : "product_kernel<lse>";
+      e = o.skinny ? launch_skinny(p, st) : launch_product(p, nullptr, st);
+    }
+    if (e == hipSuccess) e = launch_lse(o.stats, o.nstat, o.zlab, labels, classes, rows, o.lse, loss, st);
+  }
+  if (e == hipSuccess) e = launch_loss_mean(labels, classes, rows, loss, grad ? o.unit : nullptr, scale, st);
+  if (!grad || e != hipSuccess) return status(e);
+
+  // x without its padding rows, for dw: a zero gradient times what they hold
+  // need not be zero
+  if (dw) e = launch_pack(dtype, x, o.xc, rows, in, o.k.ld, labels, classes, st);
+  const long es = (long)dt_size(dtype);
+  for (long c0 = 0; c0 < classes && e == hipSuccess; c0 += o.piece) {
+    const int n = (int)std::min(o.piece, classes - c0);
+    const char* wc = (const char*)wt + c0 * o.k.ld * es;
+    if (!o.keep) {
+      Product q = p;
+      q.name = "product_kernel<dlogits>";
+      q.epi = EPI_DLOGITS;
+      q.N = n;
+      q.flops = 2.0 * rows * in * n;
+      q.a = op(xt, o.k.ld, true);
+      q.b = op(wc, o.k.ld, true);
+      q.e.bias = bias ? bias + c0 : nullptr;
+      q.e.col0 = (int)c0;
+      q.e.lse = o.lse;
+      q.e.y = o.dz;
+      q.e.ldy = o.ldd;
+      q.e.more = (bf16_t*)more;
+      q.e.rows_padded = (int)o.rows_padded;
+      q.e.colsum = db ? o.colsum : nullptr;
+      e = launch_product(q, nullptr, st);
+    } else if (db) {
+      e = launch_colsum_rows(o.logits, o.ldl, o.colsum, rows, classes, st);
+    }
+    if (e == hipSuccess && db) e = launch_colsum(o.colsum, db + c0, groups, n, accumulate, o.unit, st);
+    if (e == hipSuccess && dx) {
+      Product q;
+      q.name = "product_kernel<bwd_data>";
+      q.dt = dtype;
+      q.flops = 2.0 * rows * in * n;
+      q.M = rows;
+      q.N = in;
+      q.K = n;
+      q.a = op(o.dz, o.ldd, true);
+      q.b = op(wc, o.k.ld, false);
+      q.e.alpha = o.unit;
+      q.e.y = o.one ? dx : (void*)o.dxf;
+      q.e.out_f32 = !o.one;
+      q.e.add = !o.one && c0 > 0;
+      if (o.one) {
+        q.e.labels = labels;
+        q.e.classes = classes;
+      }
+      e = launch_product(q, o.partial, st);
+    }
+    if (e == hipSuccess && dw) {
+      Product q;
+      q.name = "product_kernel<bwd_weights>";
+      q.dt = dtype;
+      q.flops = 2.0 * rows * in * n;
+      q.M = n;
+      q.N = in;
+      q.K = split ? (int)(TERMS * o.rows_padded) : rows;
+      q.wrap = split ? (int)o.rows_padded : 0;
+      q.kb = rows;
+      q.a = op(o.dz, o.ldd, false);
+      q.b = op(o.xc, o.k.ld, false);
+      q.e.alpha = o.unit;
+      q.e.y = (char*)dw + c0 * in * (long)dt_size(dw_dtype);
+      q.e.out_f32 = dw_dtype == SINGA_F32;
+      q.e.add = accumulate != 0;
+      e = launch_product(q, o.partial, st);
+    }
+  }
+  if (e == hipSuccess && dx && !o.one) e = launch_round_rows(dtype, o.dxf, dx, rows, in, labels, classes, st);
+  return status(e);
+}
+
+size_t singa_grad_norm_workspace_bytes(int count) { return count < 0 ? 0 : norm_slots(count) * sizeof(double); }
+
+static int grad_norm(int count, const int* dtypes, const void* const* grads, void* const* outs, bool clip, const size_t* sizes,
+                     float max_norm, float* stat, void* ws, size_t ws_bytes, singa_stream stream) {
+  if (count < 0) return SINGA_ERR_SHAPE;
+  if (!(max_norm >= 0.f)) return SINGA_ERR_UNSUPPORTED;
+  if (!stat || (count && (!dtypes || !grads || !sizes || (clip && !outs)))) return SINGA_ERR_NULL;
+  for (int i = 0; i < count; ++i) {
+    if (!dtype_ok(dtypes[i])) return SINGA_ERR_UNSUPPORTED;
+    if (!sizes[i]) continue;
+    if (sizes[i] > (size_t)1 << 40) return SINGA_ERR_SHAPE;
+    if (!grads[i] || (clip && !outs[i])) return SINGA_ERR_NULL;
+    if (!aligned_to(grads[i], dt_size(dtypes[i])) || (clip && !aligned_to(outs[i], dt_size(dtypes[i])))) return SINGA_ERR_ALIGN;
+  }
+  if (!aligned_to(stat, 4)) return SINGA_ERR_ALIGN;
+  const int rc = check_ws(ws, ws_bytes, singa_grad_norm_workspace_bytes(count));
+  if (rc != SINGA_OK) return rc;
+  return status(launch_grad_norm(count, dtypes, grads, clip ? outs : nullptr, sizes, max_norm, stat, (double*)ws,
+                                 (hipStream_t)stream));
+}
+
+int singa_grad_norm(int count, const int* dtypes, const void* const* grads, const size_t* sizes, float max_norm, float* stat,
+                    void* ws, size_t ws_bytes, singa_stream stream) {
+  return grad_norm(count, dtypes, grads, nullptr, false, sizes, max_norm, stat, ws, ws_bytes, stream);
+}
+
+int singa_grad_clip(int count, const int* dtypes, const void* const* grads, void* const* outs, const size_t* sizes,
+                    float max_norm, float* stat, void* ws, size_t ws_bytes, singa_stream stream) {
+  return grad_norm(count, dtypes, grads, outs, true, sizes, max_norm, stat, ws, ws_bytes, stream);
+}
+
+int singa_sgd_momentum_update_scaled(size_t n, float* w, const float* g, float* v, uint16_t* w_bf16, float lr, float momentum,
+                                     float weight_decay, const float* grad_scale, singa_stream stream) {
+  if (n == 0) return SINGA_OK;
+  if (!w || !g || !v || !grad_scale) return SINGA_ERR_NULL;
+  if (!aligned_to(w, 16) || !aligned_to(g, 16) || !aligned_to(v, 16) || !aligned_to(w_bf16, 16) || !aligned_to(grad_scale, 4))
+    return SINGA_ERR_ALIGN;
+  return status(launch_sgd_scaled(n, w, g, v, w_bf16, lr, momentum, weight_decay, grad_scale, (hipStream_t)stream));
+}
+
+int singa_adagrad_update_scaled(size_t n, float* w, const float* g, float* h, uint16_t* w_bf16, float lr, float delta,
+                                float weight_decay, const float* grad_scale, singa_stream stream) {
+  if (n == 0) return SINGA_OK;
+  if (!w || !g || !h || !grad_scale) return SINGA_ERR_NULL;
+  if (!aligned_to(w, 16) || !aligned_to(g, 16) || !aligned_to(h, 16) || !aligned_to(w_bf16, 16) || !aligned_to(grad_scale, 4))
+    return SINGA_ERR_ALIGN;
+  if (!(delta > 0.f) || !(lr >= 0.f)) return SINGA_ERR_UNSUPPORTED;
+  return status(launch_adagrad_scaled(n, w, g, h, w_bf16, lr, delta, weight_decay, grad_scale, (hipStream_t)stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,498 @@
+// dense_aux.hip -- the dense product of few rows, and the kernels around the
+// products: operands laid out for the tiles, the gradient through an
+// activation, column sums, and the rows of a softmax cross-entropy.
+#include "dense_gemm.h"
+
+namespace singa {
+
+namespace {
+
+// ------------------------------------------------- product of few rows
+//
+// Reads B (the weights) once, 16 of its rows per workgroup, straight into
+// registers: v_mfma_f32_16x16x32_bf16 (or four v_mfma_f32_16x16x4_f32) takes
+// 16 bytes of a row from each lane, 64 consecutive bytes of a row per step, so
+// neither operand needs LDS and any row start will do (ALIGNED: 16-byte
+// loads; otherwise element loads).  The waves share the K range and add their
+// sums through LDS.  Bound by the bytes of B; U steps (U x 64 bytes of 16
+// rows) are in flight per wave.
+typedef float f32x4v __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ void mma16(const bf16x8& a, const bf16x8& b, f32x4v& c) {
+  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma16(const f32x4& a, const f32x4& b, f32x4v& c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+}
+
+// 16 bytes of a row from element k (k < K; elements from K on are zero)
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ typename Chunk<T>::type row_chunk(const T* row, int k, int K) {
+  constexpr int VEC = TypeInfo<T>::VEC;
+  if constexpr (ALIGNED) {
+    return *(const typename Chunk<T>::type*)(row + k);
+  } else {
+    union { typename Chunk<T>::type c; T e[VEC]; } u;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) u.e[j] = k + j < K ? row[k + j] : zero_elem<T>();
+    return u.c;
+  }
+}
+
+constexpr int SKINNY_WAVES = 4;
+
+template <typename T, bool ALIGNED, int MT, int EPI>
+__global__ __launch_bounds__(SKINNY_WAVES * 64) void skinny_kernel(const T* __restrict__ x, const T* __restrict__ w, int M,
+                                                                   int N, int K, Epilogue e) {
+  constexpr int VEC = TypeInfo<T>::VEC, U = MT <= 2 ? 8 : 4, STEP = 4 * VEC;
+  __shared__ float red[SKINNY_WAVES][MT * 16][16];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, li = lane & 15, kq = lane >> 4;
+  const int n0 = blockIdx.x * 16;
+  // rows past the end read the last one; their results are not used
+  const T* wr = w + (size_t)min(n0 + li, N - 1) * K;
+  const T* xr[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) xr[m] = x + (size_t)min(m * 16 + li, M - 1) * K;
+  f32x4v acc[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) acc[m] = f32x4v{0.f, 0.f, 0.f, 0.f};
+  typedef typename Chunk<T>::type C;
+  const int full = K / (STEP * U);  // runs of U whole steps
+  for (int it = wave; it < full; it += SKINNY_WAVES) {
+    const int k = it * STEP * U + kq * VEC;
+    C wc[U], xc[MT][U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) wc[u] = row_chunk<T, ALIGNED>(wr, k + u * STEP, K);
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int u = 0; u < U; ++u) xc[m][u] = row_chunk<T, ALIGNED>(xr[m], k + u * STEP, K);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) mma16(wc[u], xc[m][u], acc[m]);
+  }
+  // the remaining steps one by one; a lane past the end adds zeros
+  for (int k0 = full * STEP * U + wave * STEP; k0 < K; k0 += SKINNY_WAVES * STEP) {
+    const int k = k0 + kq * VEC;
+    C wc{}, xc[MT]{};
+    if (k < K) {
+      wc = row_chunk<T, ALIGNED>(wr, k, K);
+#pragma unroll
+      for (int m = 0; m < MT; ++m) xc[m] = row_chunk<T, ALIGNED>(xr[m], k, K);
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) mma16(wc, xc[m], acc[m]);
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m) *(f32x4v*)&red[wave][m * 16 + li][kq * 4] = acc[m];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int idx = i * 256 + threadIdx.x, row = idx >> 4, c = idx & 15, col = n0 + c;
+    float v = 0.f;
+#pragma unroll
+    for (int s = 0; s < SKINNY_WAVES; ++s) v += red[s][row][c];
+    const bool in = row < M && col < N;
+    if (e.bias && in) v += e.bias[col];
+    if constexpr (EPI == EPI_OUT) {
+      if (!in) continue;
+      const size_t o = (size_t)row * N + col;
+      if (e.z) store_out<T>((T*)e.z + o, v);
+      if (e.act) v = act_f<T>(v, e.act);
+      if (e.res) v += elem_f(((const T*)e.res)[o]);
+      if (e.out_f32)
+        ((float*)e.y)[(size_t)row * e.ldy + col] = v;
+      else
+        store_out<T>((T*)e.y + (size_t)row * e.ldy + col, v);
+    } else {
+      const float z = v;
+      v = in ? v : -INFINITY;
+      float m = v;
+#pragma unroll
+      for (int d = 1; d < 16; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+      float s = exp_fast(v - (m == -INFINITY ? 0.f : m));
+#pragma unroll
+      for (int d = 1; d < 16; d <<= 1) s += __shfl_xor(s, d);
+      if (row < M) {
+        if (c == 0) e.stats[(size_t)row * e.nstat + e.stat0 + blockIdx.x] = make_float2(m, s);
+        if (in && e.labels[row] == e.col0 + col) e.zlab[row] = z;
+      }
+    }
+  }
+}
+
+template <typename T, bool ALIGNED, int EPI> hipError_t skinny_rows(const Product& p, hipStream_t st) {
+  const dim3 grid((unsigned)((p.N + 15) / 16)), block(SKINNY_WAVES * 64);
+  const T *x = (const T*)p.a.p, *w = (const T*)p.b.p;
+  Epilogue e = p.e;
+  if (!e.ldy) e.ldy = p.N;
+  TraceScope ts(p.name, st, p.flops, WORK_FLOP);
+  switch ((p.M + 15) / 16) {
+    case 1: hipLaunchKernelGGL((skinny_kernel<T, ALIGNED, 1, EPI>), grid, block, 0, st, x, w, p.M, p.N, p.K, e); break;
+    case 2: hipLaunchKernelGGL((skinny_kernel<T, ALIGNED, 2, EPI>), grid, block, 0, st, x, w, p.M, p.N, p.K, e); break;
+    default: hipLaunchKernelGGL((skinny_kernel<T, ALIGNED, 4, EPI>), grid, block, 0, st, x, w, p.M, p.N, p.K, e); break;
+  }
+  return hipGetLastError();
+}
+
+template <typename T> hipError_t skinny_t(const Product& p, hipStream_t st) {
+  const bool aligned = p.K % TypeInfo<T>::VEC == 0;
+  if (p.epi == EPI_OUT) return aligned ? skinny_rows<T, true, EPI_OUT>(p, st) : skinny_rows<T, false, EPI_OUT>(p, st);
+  return aligned ? skinny_rows<T, true, EPI_LSE>(p, st) : skinny_rows<T, false, EPI_LSE>(p, st);
+}
+
+// ------------------------------------------------------------ operands
+template <typename T>
+__global__ __launch_bounds__(256) void pack_kernel(const T* __restrict__ in, T* __restrict__ out, long rows, int cols,
+                                                   long ldo, const int32_t* __restrict__ labels, int classes) {
+  constexpr int VEC = TypeInfo<T>::VEC;
+  const long cpr = ldo / VEC;
+  const long i = (long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= rows * cpr) return;
+  const long row = i / cpr;
+  const int c = (int)(i - row * cpr) * VEC;
+  union { uint4 u; T e[VEC]; } v;
+  v.u = make_uint4(0, 0, 0, 0);
+  if (!labels || label_ok(labels[row], classes)) {
+    const T* p = in + row * cols + c;
+    if (cols % VEC == 0) {
+      v.u = *(const uint4*)p;
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j)
+        if (c + j < cols) v.e[j] = p[j];
+    }
+  }
+  *(uint4*)(out + row * ldo + c) = v.u;
+}
+
+__global__ __launch_bounds__(256) void zero_kernel(uint16_t* p, size_t n) {
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = 0;
+}
+
+// A workgroup: COLSUM_ROWS rows of 256 columns, a thread 8 columns of every
+// eighth row.
+template <typename T>
+__global__ __launch_bounds__(256) void dact_kernel(int act, const T* __restrict__ dy, const T* __restrict__ z,
+                                                   T* __restrict__ dz, bf16_t* __restrict__ more, float* __restrict__ colsum,
+                                                   long rows, long rows_padded, int cols, long ldz) {
+  __shared__ float red[8][256];
+  const int tc = threadIdx.x & 31, tr = threadIdx.x >> 5;
+  const int col = blockIdx.y * 256 + tc * 8;
+  const long row0 = (long)blockIdx.x * COLSUM_ROWS;
+  const bool vec = cols % 8 == 0;
+  float cs[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) cs[j] = 0.f;
+  if (col < ldz) {
+#pragma unroll 2
+    for (int i = 0; i < COLSUM_ROWS / 8; ++i) {
+      const long row = row0 + i * 8 + tr;
+      if (row >= rows_padded) break;
+      float v[8], u[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = u[j] = 0.f;
+      if (row < rows) {
+        const long o = row * cols + col;
+        if (vec) {
+          load8<T>(dy + o, v);
+          if (act) load8<T>(z + o, u);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (col + j < cols) {
+              v[j] = elem_f(dy[o + j]);
+              if (act) u[j] = elem_f(z[o + j]);
+            }
+        }
+        // where ReLU passes nothing the gradient is zero, whatever dy holds
+        if (act == ACT_RELU) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = u[j] > 0.f ? v[j] : 0.f;
+        } else if (act) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] *= act_slope<T>(u[j], act);
+        }
+        if (!vec) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = col + j < cols ? v[j] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) cs[j] += v[j];
+      if (dz) store_terms<T>(dz, more, (size_t)(row * ldz + col), (size_t)(rows_padded * ldz), v);
+    }
+  }
+  if (!colsum) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) red[tr][tc * 8 + j] = cs[j];
+  __syncthreads();
+  const int c = blockIdx.y * 256 + threadIdx.x;
+  if (c >= cols || row0 >= rows) return;
+  float s = 0.f;
+#pragma unroll
+  for (int r = 0; r < 8; ++r) s += red[r][threadIdx.x];
+  colsum[(long)blockIdx.x * cols + c] = s;
+}
+
+__global__ __launch_bounds__(256) void colsum_rows_kernel(const float* __restrict__ in, long ld, float* __restrict__ colsum,
+                                                          long rows, int cols) {
+  __shared__ float red[4][64];
+  const int tc = threadIdx.x & 63, tr = threadIdx.x >> 6;
+  const int col = blockIdx.y * 64 + tc;
+  const long row0 = (long)blockIdx.x * COLSUM_ROWS;
+  float s = 0.f;
+  if (col < cols)
+    for (int i = tr; i < COLSUM_ROWS && row0 + i < rows; i += 4) s += in[(row0 + i) * ld + col];
+  red[tr][tc] = s;
+  __syncthreads();
+  if (tr == 0 && col < cols) colsum[(long)blockIdx.x * cols + col] = red[0][tc] + red[1][tc] + red[2][tc] + red[3][tc];
+}
+
+// 32 columns per workgroup, eight threads per column.
+__global__ __launch_bounds__(256) void colsum_kernel(const float* __restrict__ colsum, float* __restrict__ out, long groups,
+                                                     int cols, int add, const float* __restrict__ alpha) {
+  __shared__ float red[8][32];
+  const int tc = threadIdx.x & 31, tr = threadIdx.x >> 5, col = blockIdx.x * 32 + tc;
+  float s = 0.f;
+  if (col < cols)
+    for (long g = tr; g < groups; g += 8) s += colsum[g * cols + col];
+  red[tr][tc] = s;
+  __syncthreads();
+  if (tr || col >= cols) return;
+  s = 0.f;
+#pragma unroll
+  for (int r = 0; r < 8; ++r) s += red[r][tc];
+  if (alpha) s *= alpha[0];
+  out[col] = add ? out[col] + s : s;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void round_rows_kernel(const float* __restrict__ in, T* __restrict__ out, long rows,
+                                                         int cols, const int32_t* __restrict__ labels, int classes) {
+  const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 4;
+  const long n = rows * cols;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (i + j < n) store_out<T>(out + i + j, label_ok(labels[(i + j) / cols], classes) ? in[i + j] : 0.f);
+}
+
+// ---------------------------------------------------------------- loss rows
+// (maximum, sum of exponentials relative to it) of two sets; an empty set's
+// maximum is -inf and its sum 0.  NaN sums stay NaN.
+__device__ __forceinline__ void merge(float& m, float& s, float m2, float s2) {
+  const float mx = fmaxf(m, m2);
+  const float base = mx == -INFINITY ? 0.f : mx;
+  s = s * exp_fast(m - base) + s2 * exp_fast(m2 - base);
+  m = mx;
+}
+
+// Over W threads (a wave, or a whole workgroup of 256) that each hold a set.
+template <int W> __device__ __forceinline__ void merge_all(float& m, float& s, float2* lds) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const float m2 = __shfl_xor(m, d), s2 = __shfl_xor(s, d);
+    merge(m, s, m2, s2);
+  }
+  if constexpr (W > 64) {
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_float2(m, s);
+    __syncthreads();
+    m = lds[0].x;
+    s = lds[0].y;
+#pragma unroll
+    for (int i = 1; i < W / 64; ++i) merge(m, s, lds[i].x, lds[i].y);
+  }
+}
+
+template <int W>
+__global__ __launch_bounds__(256) void lse_kernel(const float2* __restrict__ stats, int nstat, const float* __restrict__ zlab,
+                                                  const int32_t* __restrict__ labels, int classes, long rows,
+                                                  float* __restrict__ lse, float* __restrict__ loss) {
+  __shared__ float2 lds[4];
+  const int t = threadIdx.x % W;
+  const long row = (long)blockIdx.x * (256 / W) + threadIdx.x / W;
+  if (row >= rows) return;  // whole waves (W = 64), or no workgroup at all
+  float m = -INFINITY, s = 0.f;
+  const float2* p = stats + (size_t)row * nstat;
+  for (int i = t; i < nstat; i += W) merge(m, s, p[i].x, p[i].y);
+  merge_all<W>(m, s, lds);
+  if (t == 0) {
+    const float l = m + logf(s);
+    if (lse) lse[row] = l;
+    loss[1 + row] = label_ok(labels[row], classes) ? l - zlab[row] : 0.f;
+  }
+}
+
+__device__ __forceinline__ double block_sum(double v, double* lds) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  double s = 0;
+  for (int i = 0; i < (int)blockDim.x / 64; ++i) s += lds[i];
+  __syncthreads();
+  return s;
+}
+
+// One workgroup: the mean over the counted rows, in a fixed order, and what a
+// counted row's gradient is multiplied with.
+__global__ __launch_bounds__(1024) void loss_mean_kernel(const int32_t* __restrict__ labels, int classes, long rows,
+                                                         float* __restrict__ loss, float* __restrict__ unit, float scale) {
+  __shared__ double lds[16];
+  double n = 0, s = 0;
+  for (long r = threadIdx.x; r < rows; r += 1024) {
+    const bool ok = label_ok(labels[r], classes);
+    n += ok;
+    if (ok) s += loss[1 + r];
+  }
+  n = block_sum(n, lds);
+  s = block_sum(s, lds);
+  if (threadIdx.x) return;
+  loss[0] = n > 0 ? (float)(s / n) : 0.f;
+  if (unit) unit[0] = n > 0 ? (float)(scale / n) : 0.f;
+}
+
+// W threads per row of kept logits; dzf may be z itself.
+template <typename T, int W>
+__global__ __launch_bounds__(256) void loss_rows_kernel(const float* z, long ldz, const int32_t* __restrict__ labels,
+                                                        long rows, long rows_padded, int classes,
+                                                        float* __restrict__ loss, T* __restrict__ dz, bf16_t* __restrict__ more,
+                                                        long ldd, float* dzf) {
+  __shared__ float2 lds[4];
+  const int t = threadIdx.x % W;
+  const long row = (long)blockIdx.x * (256 / W) + threadIdx.x / W;
+  if (row >= rows_padded) return;
+  const int lab = row < rows ? labels[row] : -1;
+  const bool live = label_ok(lab, classes);
+  const float* zr = z + (size_t)(row < rows ? row : 0) * ldz;
+  float lse = 0.f;
+  if (live) {  // the same for all threads of a row
+    float m = -INFINITY, s = 0.f;
+    for (int c = t; c < classes; c += W) m = fmaxf(m, zr[c]);
+    const float base = m == -INFINITY ? 0.f : m;
+    for (int c = t; c < classes; c += W) s += exp_fast(zr[c] - base);
+    merge_all<W>(m, s, lds);
+    lse = m + logf(s);
+  }
+  if (t == 0 && row < rows) loss[1 + row] = live ? lse - zr[lab] : 0.f;
+  if (!dz) return;
+  if constexpr (W > 64) __syncthreads();  // the label's logit is read before dzf overwrites it
+  for (long c = t; c < ldd; c += W) {
+    float v = 0.f;
+    if (live && c < classes) v = exp_fast(zr[c] - lse) - (c == lab ? 1.f : 0.f);
+    store_out<T>(dz + row * ldd + c, v);
+    if (sizeof(T) == 2 && more) {
+      float left = v;
+      for (int i = 0; i < TERMS - 1; ++i) {
+        left -= bf16_to_f32(f32_to_bf16(left));
+        more[(i * rows_padded + row) * ldd + c] = f32_to_bf16(left);
+      }
+    }
+    if (dzf && row < rows && c < classes) dzf[row * ldz + c] = v;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_zero(void* p, size_t bytes, hipStream_t st) {
+  TraceScope ts("zero_kernel", st, (double)bytes, WORK_BYTE);
+  const size_t n = bytes / 2, wgs = (n + 255) / 256;
+  hipLaunchKernelGGL(zero_kernel, dim3((unsigned)(wgs < 4096 ? wgs : 4096)), dim3(256), 0, st, (uint16_t*)p, n);
+  return hipGetLastError();
+}
+
+hipError_t launch_skinny(const Product& p, hipStream_t st) { return p.dt == BF16 ? skinny_t<bf16_t>(p, st) : skinny_t<float>(p, st); }
+
+hipError_t launch_pack(int dt, const void* in, void* out, long rows, int cols, long ldo, const int32_t* labels, int classes,
+                       hipStream_t st) {
+  TraceScope ts("pack_kernel", st, (double)rows * (cols + ldo) * dt_size(dt), WORK_BYTE);
+  if (dt == BF16)
+    hipLaunchKernelGGL(pack_kernel<bf16_t>, dim3((unsigned)((rows * (ldo / 8) + 255) / 256)), dim3(256), 0, st,
+                       (const bf16_t*)in, (bf16_t*)out, rows, cols, ldo, labels, classes);
+  else
+    hipLaunchKernelGGL(pack_kernel<float>, dim3((unsigned)((rows * (ldo / 4) + 255) / 256)), dim3(256), 0, st,
+                       (const float*)in, (float*)out, rows, cols, ldo, labels, classes);
+  return hipGetLastError();
+}
+
+hipError_t launch_dact(int dt, int act, const void* dy, const void* z, void* dz, void* more, float* colsum, long rows,
+                       long rows_padded, int cols, long ldz, hipStream_t st) {
+  const dim3 grid((unsigned)((rows_padded + COLSUM_ROWS - 1) / COLSUM_ROWS), (unsigned)((ldz + 255) / 256));
+  TraceScope ts("dact_kernel", st, (double)rows * cols * dt_size(dt) * (1 + (act != 0) + (dz != nullptr) + (more ? TERMS - 1 : 0)),
+                WORK_BYTE);
+  if (dt == BF16)
+    hipLaunchKernelGGL(dact_kernel<bf16_t>, grid, dim3(256), 0, st, act, (const bf16_t*)dy, (const bf16_t*)z, (bf16_t*)dz,
+                       (bf16_t*)more, colsum, rows, rows_padded, cols, ldz);
+  else
+    hipLaunchKernelGGL(dact_kernel<float>, grid, dim3(256), 0, st, act, (const float*)dy, (const float*)z, (float*)dz,
+                       (bf16_t*)nullptr, colsum, rows, rows_padded, cols, ldz);
+  return hipGetLastError();
+}
+
+hipError_t launch_colsum(const float* colsum, float* out, long groups, int cols, int add, const float* alpha, hipStream_t st) {
+  TraceScope ts("colsum_kernel", st, 4.0 * groups * cols, WORK_BYTE);
+  hipLaunchKernelGGL(colsum_kernel, dim3((unsigned)((cols + 31) / 32)), dim3(256), 0, st, colsum, out, groups, cols, add,
+                     alpha);
+  return hipGetLastError();
+}
+
+hipError_t launch_colsum_rows(const float* dzf, long ld, float* colsum, long rows, int cols, hipStream_t st) {
+  TraceScope ts("colsum_rows_kernel", st, 4.0 * rows * cols, WORK_BYTE);
+  const dim3 grid((unsigned)((rows + COLSUM_ROWS - 1) / COLSUM_ROWS), (unsigned)((cols + 63) / 64));
+  hipLaunchKernelGGL(colsum_rows_kernel, grid, dim3(256), 0, st, dzf, ld, colsum, rows, cols);
+  return hipGetLastError();
+}
+
+hipError_t launch_round_rows(int dt, const float* in, void* out, long rows, int cols, const int32_t* labels, int classes,
+                             hipStream_t st) {
+  TraceScope ts("round_rows_kernel", st, (double)rows * cols * (4 + dt_size(dt)), WORK_BYTE);
+  const dim3 grid((unsigned)((rows * cols + 1023) / 1024));
+  if (dt == BF16)
+    hipLaunchKernelGGL(round_rows_kernel<bf16_t>, grid, dim3(256), 0, st, in, (bf16_t*)out, rows, cols, labels, classes);
+  else
+    hipLaunchKernelGGL(round_rows_kernel<float>, grid, dim3(256), 0, st, in, (float*)out, rows, cols, labels, classes);
+  return hipGetLastError();
+}
+
+hipError_t launch_lse(const float2* stats, int nstat, const float* zlab, const int32_t* labels, int classes, long rows,
+                      float* lse, float* loss, hipStream_t st) {
+  TraceScope ts("lse_kernel", st, 8.0 * rows * nstat, WORK_BYTE);
+  // a wave per row, or, where rows are few, a workgroup per row
+  if (rows >= 1024)
+    hipLaunchKernelGGL(lse_kernel<64>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, stats, nstat, zlab, labels, classes,
+                       rows, lse, loss);
+  else
+    hipLaunchKernelGGL(lse_kernel<256>, dim3((unsigned)rows), dim3(256), 0, st, stats, nstat, zlab, labels, classes, rows, lse,
+                       loss);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_mean(const int32_t* labels, int classes, long rows, float* loss, float* unit, float scale,
+                            hipStream_t st) {
+  TraceScope ts("loss_mean_kernel", st, 8.0 * rows, WORK_BYTE);
+  hipLaunchKernelGGL(loss_mean_kernel, dim3(1), dim3(1024), 0, st, labels, classes, rows, loss, unit, scale);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_rows(int dt, const float* z, long ldz, const int32_t* labels, long rows, long rows_padded, int classes,
+                            float* loss, void* dz, void* more, long ldd, float* dzf, hipStream_t st) {
+  TraceScope ts("loss_rows_kernel", st, (double)rows * classes * (8 + dt_size(dt)), WORK_BYTE);
+  const bool wide = classes > 1024;  // a workgroup per row, else a wave
+  const dim3 grid((unsigned)(wide ? rows_padded : (rows_padded + 3) / 4));
+#define SINGA_ROWS(T, W)                                                                                                     \
+  hipLaunchKernelGGL((loss_rows_kernel<T, W>), grid, dim3(256), 0, st, z, ldz, labels, rows, rows_padded, classes, loss, \
+                     (T*)dz, (bf16_t*)more, ldd, dzf)
+  if (dt == BF16) {
+    if (wide) SINGA_ROWS(bf16_t, 256);
+    else SINGA_ROWS(bf16_t, 64);
+  } else {
+    if (wide) SINGA_ROWS(float, 256);
+    else SINGA_ROWS(float, 64);
+  }
+#undef SINGA_ROWS
+  return hipGetLastError();
+}
+
+}  // namespace singa

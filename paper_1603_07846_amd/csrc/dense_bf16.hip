@@ -1,0 +1,10 @@
+// dense_bf16.hip -- the dense products of bf16 operands (dense_gemm.h).
+#include "dense_gemm.h"
+
+namespace singa {
+
+hipError_t launch_product_bf16(const Product& p, float* partial, hipStream_t st) {
+  return launch_product_t<bf16_t>(p, partial, st);
+}
+
+}  // namespace singa

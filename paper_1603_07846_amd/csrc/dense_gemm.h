@@ -1,0 +1,586 @@
+// dense_gemm.h -- the tile kernel of the dense products (see dense.h).
+//
+// A workgroup computes a BM x BN tile; the K range goes through LDS in tiles
+// of 128 bytes (64 bf16 or 32 fp32 values of k), written there straight from
+// memory (buffer loads to LDS) two stages deep.  An operand is staged the way
+// it is stored:
+//   K contiguous:    BM rows of 128 bytes; a lane's fragment (8 bf16 or 4 fp32
+//                    of one row) is one 16-byte read.  16-byte chunk c of row
+//                    r lies in slot c ^ (r / 2 % 8), so that 16 rows read at
+//                    the same k touch 16 different 16-byte groups of banks.
+//   rows contiguous: 64 (32) rows of k; bf16 fragments come from transposing
+//                    LDS reads (four k of 16 rows each), fp32 ones from four
+//                    4-byte reads.  Chunk c of k row d lies in slot
+//                    c ^ 4 (d % 4) (bf16) or c ^ 8 (d / 4 % 2) (fp32): the
+//                    rows that one read touches lie in different banks.
+// Both operands take their k in the same order, so either type's fragments
+// feed the matrix instruction as they come: v_mfma_f32_32x32x16_bf16 once or
+// v_mfma_f32_32x32x2_f32 four times per 16 bytes.  Sums are fp32.
+#pragma once
+
+#include "conv_common.h"
+#include "dense.h"
+
+namespace singa {
+
+namespace {
+
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+struct GemmArgs {
+  const char *a, *b;
+  long lda, ldb;            // bytes
+  long enda, endb;          // bytes of the whole operand
+  int M, N;
+  int kca, kcb;             // 16-byte chunks of K (K contiguous operands)
+  int kt_all, kt_split, splits, wrap;  // K-tiles: all, per split, splits, where B starts again (0: never)
+  int tiles_m, tiles_n;
+  float* partial;           // [splits][M][ldp] when splits > 1
+  long ldp;
+  int vec;                  // outputs take 16-byte vectors
+  Epilogue e;
+};
+
+__device__ __forceinline__ v4i16 lds_tr16(const char* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (__attribute__((address_space(3))) v4i16*)(__attribute__((address_space(3))) char*)p);
+}
+
+// exp in the hardware's base-2 form: x log2(e) is rounded once, so the result
+// is off by at most |x| 2^-24 relative (x <= 0 here, and what matters of a
+// softmax lies at small |x|) besides the instruction's own ulp.
+__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+
+// erfc(x) for x >= 0, without the factor exp(-x^2): Abramowitz and Stegun
+// 7.1.26, absolute error of the product below 1.5e-7.
+__device__ __forceinline__ float erfc_poly(float x) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
+  return t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+}
+
+// act(z).  bf16 results need 2^-9: the hardware's exponential and reciprocal
+// and the polynomial do; fp32 results take the library's functions.
+template <typename T> __device__ __forceinline__ float act_f(float z, int act) {
+  constexpr bool FAST = sizeof(T) == 2;
+  if (act == ACT_RELU) return z > 0.f ? z : (z != z ? z : 0.f);
+  if (act == ACT_GELU) {
+    if constexpr (FAST) {
+      const float u = fabsf(z) * 0.70710678118654752f;
+      const float h = 0.5f * erfc_poly(u) * exp_fast(-u * u);
+      return z * (z < 0.f ? h : 1.f - h);
+    }
+    return 0.5f * z * erfcf(-z * 0.70710678118654752f);
+  }
+  if (act == ACT_SILU) {
+    if constexpr (FAST) return z * __builtin_amdgcn_rcpf(1.f + exp_fast(-z));
+    return z / (1.f + expf(-z));
+  }
+  return z;
+}
+
+// act'(z): dz = dy act'(z)
+template <typename T> __device__ __forceinline__ float act_slope(float z, int act) {
+  if (act == ACT_RELU) return z > 0.f ? 1.f : 0.f;
+  if (act == ACT_GELU) return fmaf(z * 0.39894228040143268f, expf(-0.5f * z * z), 0.5f * erfcf(-z * 0.70710678118654752f));
+  if (act == ACT_SILU) {
+    const float s = 1.f / (1.f + expf(-z));
+    return s * fmaf(z, 1.f - s, 1.f);
+  }
+  return 1.f;
+}
+
+// ------------------------------------------------------------- epilogues
+template <typename T> __device__ __forceinline__ void load8(const T* p, float (&v)[8]);
+template <> __device__ __forceinline__ void load8<float>(const float* p, float (&v)[8]) {
+  const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = a[j], v[4 + j] = b[j];
+}
+template <> __device__ __forceinline__ void load8<bf16_t>(const bf16_t* p, float (&v)[8]) {
+  const uint4 u = *(const uint4*)p;
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[2 * j] = __uint_as_float(w[j] << 16);
+    v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+  }
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, const float (&v)[8]);
+template <> __device__ __forceinline__ void store8<float>(float* p, const float (&v)[8]) {
+  *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+  *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+}
+template <> __device__ __forceinline__ void store8<bf16_t>(bf16_t* p, const float (&v)[8]) {
+  *(u32x4_t*)p = u32x4_t{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]),
+                         f32x2_to_bf16x2(v[6], v[7])};
+}
+
+// v at y + o and, with more, its further terms, `step` elements apart.
+template <typename T>
+__device__ __forceinline__ void store_terms(T* y, bf16_t* more, size_t o, size_t step, float (&v)[8]) {
+  store8<T>(y + o, v);
+  if constexpr (sizeof(T) == 2) {
+    if (more) {
+#pragma unroll
+      for (int t = 0; t < TERMS - 1; ++t) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] -= bf16_to_f32(f32_to_bf16(v[j]));
+        store8<bf16_t>(more + t * step + o, v);
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ bool label_ok(int lab, int classes) { return lab >= 0 && lab < classes; }
+
+// EPI_OUT on 8 columns from col of one row; vec: N % 8 == 0 and every tensor
+// starts at a 16-byte boundary.
+template <typename T>
+__device__ __forceinline__ void epi_out(const Epilogue& e, int N, bool vec, int row, int col, float (&v)[8]) {
+  const size_t o = (size_t)row * N + col;
+  const size_t oy = (size_t)row * e.ldy + col;
+  const bool live = !e.labels || label_ok(e.labels[row], e.classes);
+  const int n = min(8, N - col);
+  if (e.alpha) {
+    const float alpha = e.alpha[0];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= alpha;
+  }
+  if (e.bias) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) v[j] += e.bias[col + j];
+  }
+  if (vec) {
+    if (e.z) store8<T>((T*)e.z + o, v);
+    if (e.act) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = act_f<T>(v[j], e.act);
+    }
+    if (e.res) {
+      float r[8];
+      load8<T>((const T*)e.res + o, r);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += r[j];
+    }
+    if (!live) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    }
+    if (e.out_f32) {
+      float* y = (float*)e.y + oy;
+      if (e.add) {
+        float r[8];
+        load8<float>(y, r);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += r[j];
+      }
+      store8<float>(y, v);
+    } else {
+      store8<T>((T*)e.y + oy, v);
+    }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    if (j >= n) break;
+    float x = v[j];
+    if (e.z) store_out<T>((T*)e.z + o + j, x);
+    if (e.act) x = act_f<T>(x, e.act);
+    if (e.res) x += elem_f(((const T*)e.res)[o + j]);
+    if (!live) x = 0.f;
+    if (e.out_f32) {
+      float* y = (float*)e.y + oy + j;
+      *y = e.add ? *y + x : x;
+    } else {
+      store_out<T>((T*)e.y + oy + j, x);
+    }
+  }
+}
+
+template <typename T> struct TypeInfo;
+template <> struct TypeInfo<bf16_t> {
+  static constexpr int VEC = 8, BK = 64;
+};
+template <> struct TypeInfo<float> {
+  static constexpr int VEC = 4, BK = 32;
+};
+
+template <typename T> struct Chunk;
+template <> struct Chunk<bf16_t> { typedef bf16x8 type; };
+template <> struct Chunk<float> { typedef f32x4 type; };
+
+__device__ __forceinline__ void mma32(const bf16x8& a, const bf16x8& b, f32x16& c) {
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma32(const f32x4& a, const f32x4& b, f32x16& c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+}
+
+// One operand's tile: R rows of the product by one K-tile, in LDS, with NW
+// waves loading it.  W0: the first of this wave's rows.
+template <typename T, bool KC, int R, int NW> struct Tile {
+  static constexpr int ES = (int)sizeof(T), VEC = TypeInfo<T>::VEC, BK = TypeInfo<T>::BK;
+  static constexpr int BYTES = R * 128;
+  static constexpr int NI = BYTES / 1024 / NW;  // load instructions per wave and K-tile
+  static_assert(BYTES % (1024 * NW) == 0, "whole instructions");
+  static constexpr int RB = R * ES;             // rows contiguous: bytes of a k row
+  static constexpr int CPR = RB / 16;
+
+  uint32_t off[NI];  // within the tile's rsrc; OOB: nothing to read
+  int kch[NI];       // K contiguous: the chunk's k position within the K-tile
+
+  __device__ __forceinline__ void init(int wave, int lane, long ld, int r0, int rows) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int idx = wave * NI + i;
+      if constexpr (KC) {
+        const int r = idx * 8 + (lane >> 3);
+        kch[i] = (lane & 7) ^ ((r >> 1) & 7);
+        off[i] = r0 + r < rows ? (uint32_t)(r * ld + kch[i] * 16) : OOB;
+      } else {
+        constexpr int RPI = 1024 / RB;
+        const int d = idx * RPI + lane / CPR;
+        const int c = (lane % CPR) ^ (ES == 2 ? 4 * (d & 3) : 8 * ((d >> 2) & 1));
+        off[i] = r0 + c * VEC < (rows + VEC - 1) / VEC * VEC ? (uint32_t)(d * ld + c * 16) : OOB;
+        kch[i] = d;
+      }
+    }
+  }
+  // the rsrc of K-tile kt: the tile's corner, and the bytes from there to the
+  // operand's end
+  __device__ __forceinline__ static __amdgpu_buffer_rsrc_t rsrc(const char* p, long ld, long end, int r0, int kt) {
+    const long at = KC ? (long)r0 * ld + (long)kt * 128 : (long)kt * BK * ld + (long)r0 * ES;
+    const long left = end - at;
+    const uint32_t n = left <= 0 ? 0u : left > 0x7ffffff0L ? 0x7ffffff0u : (uint32_t)left;
+    return make_rsrc(p + (left <= 0 ? 0 : at), n);
+  }
+  // kleft: K contiguous: chunks of K from this K-tile on
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, char* lds, int wave, int i, int kleft) const {
+    const uint32_t o = KC ? (kch[i] < kleft ? off[i] : OOB) : off[i];
+    ld_lds16_asm(rs, o, lds + (wave * NI + i) * 1024);
+  }
+};
+
+// Fragment reads of one operand for a wave: F blocks of 32 rows from w0.
+template <typename T, bool KC, int R, int F> struct Frags {
+  static constexpr int ES = (int)sizeof(T);
+  static constexpr int RB = R * ES;
+  int addr[KC ? 4 : F];
+  __device__ __forceinline__ void init(int lane, int w0) {
+    const int li = lane & 31, lh = lane >> 5;
+    if constexpr (KC) {
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) addr[ks] = (w0 + li) * 128 + (((2 * ks + lh) ^ ((li >> 1) & 7)) << 4);
+    } else if constexpr (ES == 2) {
+      const int row = 8 * lh + ((lane & 15) >> 2), rr = row & 3;
+      const int low = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), odd = 8 * (lane & 1);
+#pragma unroll
+      for (int b = 0; b < F; ++b) addr[b] = row * RB + ((4 * ((w0 / 32 + b) ^ rr) + low) << 4) + odd;
+    } else {
+#pragma unroll
+      for (int b = 0; b < F; ++b) {
+        const int col = w0 + b * 32 + li;
+        addr[b] = 4 * lh * RB + (((col >> 2) ^ (8 * lh)) << 4) + (col & 3) * 4;
+      }
+    }
+  }
+  __device__ __forceinline__ typename Chunk<T>::type read(const char* s, int b, int ks) const {
+    if constexpr (KC) {
+      return *(const typename Chunk<T>::type*)(s + addr[ks] + b * 32 * 128);
+    } else if constexpr (ES == 2) {
+      const v4i16 lo = lds_tr16(s + addr[b] + ks * 16 * RB);
+      const v4i16 hi = lds_tr16(s + addr[b] + (ks * 16 + 4) * RB);
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      f32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = *(const float*)(s + addr[b] + (ks * 8 + e) * RB);
+      return v;
+    }
+  }
+};
+
+// WM x WN waves of (32 FM) x (32 FN).
+template <typename T, bool AKC, bool BKC, int WM, int WN, int FM, int FN, int EPI>
+__global__ __launch_bounds__(WM* WN * 64) void product_kernel(GemmArgs g) {
+  constexpr int NW = WM * WN, BM = WM * FM * 32, BN = WN * FN * 32;
+  typedef Tile<T, AKC, BM, NW> TA;
+  typedef Tile<T, BKC, BN, NW> TB;
+  constexpr int STAGE = TA::BYTES + TB::BYTES;
+  constexpr int PIT = FN * 32 + 8;  // floats per staged row: rows 4 apart lie half the banks apart
+  constexpr int SMEM = 2 * STAGE > NW * 32 * PIT * 4 ? 2 * STAGE : NW * 32 * PIT * 4;
+  __shared__ __align__(1024) char smem[SMEM];
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  // tiles in groups of 8 tile rows, column by column, dealt to the XCDs in
+  // contiguous runs: neighbours share operand rows in one L2
+  const int tiles = g.tiles_m * g.tiles_n;
+  const int split = blockIdx.x / tiles;
+  int t = xcd_remap(blockIdx.x - split * tiles, tiles);
+  constexpr int GM = 8;
+  const int group = t / (GM * g.tiles_n), first = group * GM, gm = min(GM, g.tiles_m - first);
+  t -= group * GM * g.tiles_n;
+  const int tm = first + t % gm, tn = t / gm;
+  const int m0 = tm * BM, n0 = tn * BN;
+
+  const int wm = wave / WN, wn = wave % WN;
+  TA ta;
+  TB tb;
+  ta.init(wave, lane, g.lda, m0, g.M);
+  tb.init(wave, lane, g.ldb, n0, g.N);
+  Frags<T, AKC, BM, FM> fa;
+  Frags<T, BKC, BN, FN> fb;
+  fa.init(lane, wm * FM * 32);
+  fb.init(lane, wn * FN * 32);
+
+  f32x16 acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+
+  const int kt0 = split * g.kt_split, kt1 = min(g.kt_all, kt0 + g.kt_split);
+  auto issue = [&](int kt, char* s) {
+    int kb = kt;  // the K-tile of B
+    static_assert(TERMS == 3, "two places where B starts again");
+    if (g.wrap && kb >= g.wrap) kb -= g.wrap;
+    if (g.wrap && kb >= g.wrap) kb -= g.wrap;
+    const auto ra = TA::rsrc(g.a, g.lda, g.enda, m0, kt);
+    const auto rb = TB::rsrc(g.b, g.ldb, g.endb, n0, kb);
+#pragma unroll
+    for (int i = 0; i < TA::NI; ++i) ta.load(ra, s, wave, i, g.kca - kt * 8);
+#pragma unroll
+    for (int i = 0; i < TB::NI; ++i) tb.load(rb, s + TA::BYTES, wave, i, g.kcb - kb * 8);
+  };
+  if (kt0 < kt1) issue(kt0, smem);
+  int stage = 0;
+  for (int kt = kt0; kt < kt1; ++kt) {
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0): this K-tile has landed for this wave, its LDS reads are done
+    block_barrier();  // ... and for everyone, and everyone is done with the other stage
+    if (kt + 1 < kt1) issue(kt + 1, smem + (stage ^ 1) * STAGE);
+    const char* s = smem + stage * STAGE;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      typename Chunk<T>::type af[FM], bf[FN];
+#pragma unroll
+      for (int b = 0; b < FM; ++b) af[b] = fa.read(s, b, ks);
+#pragma unroll
+      for (int b = 0; b < FN; ++b) bf[b] = fb.read(s + TA::BYTES, b, ks);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) mma32(af[i], bf[j], acc[i][j]);
+    }
+    stage ^= 1;
+  }
+  __syncthreads();  // everyone is done with the operand tiles
+
+  // Each block of 32 rows goes through the wave's own LDS region, so that a
+  // lane holds 8 consecutive columns of a row.
+  float* const q = (float*)(smem + wave * 32 * PIT * 4);
+  constexpr int LPR = FN * 4;        // lanes per row
+  constexpr int RPP = 64 / LPR;      // rows per pass
+  const int li = lane & 31, lh = lane >> 5;
+  const int c8 = (lane % LPR) * 8, rr = lane / LPR;
+  const int col = n0 + wn * FN * 32 + c8;
+  float bv[8], cs[8];
+  if constexpr (EPI != EPI_OUT) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      bv[j] = g.e.bias && col + j < g.N ? g.e.bias[col + j] : 0.f;
+      cs[j] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int bm = 0; bm < FM; ++bm) {
+    const int row0 = m0 + (wm * FM + bm) * 32;
+#pragma unroll
+    for (int bn = 0; bn < FN; ++bn)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) q[(8 * (v >> 2) + 4 * lh + (v & 3)) * PIT + bn * 32 + li] = acc[bm][bn][v];
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's LDS writes are done
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    for (int pass = 0; pass < 32 / RPP; ++pass) {
+      const int r = pass * RPP + rr, row = row0 + r;
+      float v[8];
+      load8<float>(q + r * PIT + c8, v);
+      if constexpr (EPI == EPI_OUT) {
+        if (row < g.M && col < g.N) {
+          if (g.splits > 1)
+            store8<float>(g.partial + ((size_t)split * g.M + row) * g.ldp + col, v);
+          else
+            epi_out<T>(g.e, g.N, g.vec, row, col, v);
+        }
+      } else if constexpr (EPI == EPI_LSE) {
+        static_assert(EPI != EPI_LSE || FN * 32 == STAT_COLS, "a wave's columns are one group");
+        float m = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          v[j] = col + j < g.N ? v[j] + bv[j] : -INFINITY;
+          m = fmaxf(m, v[j]);
+        }
+#pragma unroll
+        for (int d = 1; d < LPR; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+        const float ms = m == -INFINITY ? 0.f : m;
+        float s = 0.f;  // NaN where a value is (fmaxf passed over it)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += exp_fast(v[j] - ms);
+#pragma unroll
+        for (int d = 1; d < LPR; d <<= 1) s += __shfl_xor(s, d);
+        if (row < g.M) {
+          if (c8 == 0 && col < g.N) g.e.stats[(size_t)row * g.e.nstat + g.e.stat0 + col / STAT_COLS] = make_float2(m, s);
+          const int lab = g.e.labels[row];
+          const uint32_t at = (uint32_t)lab - (uint32_t)(g.e.col0 + col);
+          if (at < 8u && label_ok(lab, g.e.classes)) {
+            float z = v[0];
+#pragma unroll
+            for (int j = 1; j < 8; ++j) z = at == (uint32_t)j ? v[j] : z;
+            g.e.zlab[row] = z;
+          }
+        }
+      } else {
+        const int lab = row < g.M ? g.e.labels[row] : -1;
+        const bool live = label_ok(lab, g.e.classes);
+        const float lse = live ? g.e.lse[row] : 0.f;
+        const uint32_t at = (uint32_t)lab - (uint32_t)(g.e.col0 + col);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float p = exp_fast(v[j] + bv[j] - lse) - (at == (uint32_t)j ? 1.f : 0.f);
+          v[j] = live && col + j < g.N ? p : 0.f;
+          cs[j] += v[j];
+        }
+        if (row < g.e.rows_padded && col < g.e.ldy) {
+          store_terms<T>((T*)g.e.y, g.e.more, (size_t)row * g.e.ldy + col, (size_t)g.e.rows_padded * g.e.ldy, v);
+        }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+    if constexpr (EPI == EPI_DLOGITS) {
+      if (((bm + 1) * 32) % COLSUM_ROWS == 0) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+#pragma unroll
+          for (int d = LPR; d < 64; d <<= 1) cs[j] += __shfl_xor(cs[j], d);
+        }
+        const int row = row0 + 32 - COLSUM_ROWS;
+        if (g.e.colsum && rr == 0 && row < g.M) {
+          float* out = g.e.colsum + (size_t)(row / COLSUM_ROWS) * g.N + col;
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (col + j < g.N) out[j] = cs[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) cs[j] = 0.f;
+      }
+    }
+  }
+}
+
+// Adds the partial sums of a split product in order and finishes them.
+template <typename T> __global__ __launch_bounds__(256) void product_reduce_kernel(GemmArgs g) {
+  const int n8 = (int)(g.ldp / 8);
+  const long i = (long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (long)g.M * n8) return;
+  const int row = (int)(i / n8), col = (int)(i - (long)row * n8) * 8;
+  float v[8];
+  const float* p = g.partial + (size_t)row * g.ldp + col;
+  const size_t step = (size_t)g.M * g.ldp;
+  load8<float>(p, v);
+  for (int s = 1; s < g.splits; ++s) {
+    float u[8];
+    load8<float>(p + s * step, u);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += u[j];
+  }
+  epi_out<T>(g.e, g.N, g.vec, row, col, v);
+}
+
+struct Plan {
+  int big, splits, kt_split;
+};
+
+// 256 x 256 tiles (bf16) where they fill most of the chip; otherwise 128 x 128
+// ones, and, where those are fewer than the workgroups that run at once, the K
+// range cut so that about 512 run, each with at least 8 K-tiles.
+inline Plan plan_product(int dt, int M, int N, int K, int epi) {
+  auto up = [](long a, long b) { return (a + b - 1) / b; };
+  const int bk = dt == BF16 ? 64 : 32;
+  const int kt = (int)up(K, bk);
+  Plan p{0, 1, kt};
+  if (dt == BF16 && up(M, 256) * up(N, 256) >= 192) {
+    p.big = 1;
+    return p;
+  }
+  const long tiles = up(M, 128) * up(N, 128);
+  if (epi == EPI_OUT && tiles < 256) {
+    long s = 512 / tiles;
+    if (s > kt / 8) s = kt / 8;
+    if (s > 32) s = 32;
+    if (s > 1) {
+      p.kt_split = (int)up(kt, s);
+      p.splits = (int)up(kt, p.kt_split);
+    }
+  }
+  return p;
+}
+
+template <typename T, bool AKC, bool BKC, int EPI> hipError_t launch_tiles(const Product& p, const GemmArgs& g, bool big, hipStream_t st) {
+  const dim3 grid((unsigned)((long)g.tiles_m * g.tiles_n * g.splits));
+  TraceScope ts(p.name, st, p.flops, WORK_FLOP);
+  if (sizeof(T) == 2 && big)
+    hipLaunchKernelGGL((product_kernel<T, AKC, BKC, 2, 4, sizeof(T) == 2 ? 4 : 2, 2, EPI>), grid, dim3(512), 0, st, g);
+  else
+    hipLaunchKernelGGL((product_kernel<T, AKC, BKC, 2, 2, 2, 2, EPI>), grid, dim3(256), 0, st, g);
+  return hipGetLastError();
+}
+
+template <typename T> hipError_t launch_product_t(const Product& p, float* partial, hipStream_t st) {
+  constexpr int ES = (int)sizeof(T), VEC = TypeInfo<T>::VEC;
+  const Plan pl = plan_product(p.dt, p.M, p.N, p.K, p.epi);
+  const int bm = pl.big ? 256 : 128;
+  GemmArgs g{};
+  const long kb = p.kb ? p.kb : p.K;
+  g.a = (const char*)p.a.p;
+  g.b = (const char*)p.b.p;
+  g.lda = p.a.ld * ES;
+  g.ldb = p.b.ld * ES;
+  g.enda = (p.a.kc ? (long)p.M : (long)p.K) * g.lda;
+  g.endb = (p.b.kc ? (long)p.N : kb) * g.ldb;
+  g.M = p.M;
+  g.N = p.N;
+  g.kca = g.kcb = (p.K + VEC - 1) / VEC;
+  g.kt_all = (p.K + TypeInfo<T>::BK - 1) / TypeInfo<T>::BK;
+  g.kt_split = pl.kt_split;
+  g.splits = pl.splits;
+  g.wrap = p.wrap / TypeInfo<T>::BK;
+  g.tiles_m = (p.M + bm - 1) / bm;
+  g.tiles_n = (p.N + bm - 1) / bm;
+  g.partial = partial;
+  g.ldp = ((long)p.N + 7) / 8 * 8;
+  g.vec = p.N % 8 == 0;
+  g.e = p.e;
+  if (!g.e.ldy) g.e.ldy = p.N;
+  hipError_t e = hipErrorNotSupported;
+  if (p.epi == EPI_OUT) {
+    if (p.a.kc && p.b.kc) e = launch_tiles<T, true, true, EPI_OUT>(p, g, pl.big, st);
+    if (p.a.kc && !p.b.kc) e = launch_tiles<T, true, false, EPI_OUT>(p, g, pl.big, st);
+    if (!p.a.kc && !p.b.kc) e = launch_tiles<T, false, false, EPI_OUT>(p, g, pl.big, st);
+  } else if (p.a.kc && p.b.kc) {
+    e = p.epi == EPI_LSE ? launch_tiles<T, true, true, EPI_LSE>(p, g, pl.big, st)
+                         : launch_tiles<T, true, true, EPI_DLOGITS>(p, g, pl.big, st);
+  }
+  if (e != hipSuccess || g.splits == 1) return e;
+  TraceScope ts("product_reduce_kernel", st, 4.0 * (g.splits + 1) * p.M * p.N, WORK_BYTE);
+  hipLaunchKernelGGL(product_reduce_kernel<T>, dim3((unsigned)(((long)p.M * (g.ldp / 8) + 255) / 256)), dim3(256), 0, st, g);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+}  // namespace singa

@@ -640,6 +640,22 @@ __global__ __launch_bounds__(256) void adagrad_kernel(size_t n, float* __restric
   update_stream(n, w, g, h, wb, [=](float& we, float& he, float ge) { adagrad_step(we, he, ge, lr, delta, wd); });
 }
 
+// The same with the gradient multiplied by a factor in device memory (a global
+// norm's clipping scale): read once per thread, beside the streams.
+__global__ __launch_bounds__(256) void sgd_scaled_kernel(size_t n, float* __restrict__ w, const float* __restrict__ g,
+                                                         float* __restrict__ v, uint16_t* __restrict__ wb, float lr,
+                                                         float mom, float wd, const float* __restrict__ scale) {
+  const float s = scale[0];
+  update_stream(n, w, g, v, wb, [=](float& we, float& ve, float ge) { sgd_step(we, ve, s * ge, lr, mom, wd); });
+}
+
+__global__ __launch_bounds__(256) void adagrad_scaled_kernel(size_t n, float* __restrict__ w, const float* __restrict__ g,
+                                                             float* __restrict__ h, uint16_t* __restrict__ wb, float lr,
+                                                             float delta, float wd, const float* __restrict__ scale) {
+  const float s = scale[0];
+  update_stream(n, w, g, h, wb, [=](float& we, float& he, float ge) { adagrad_step(we, he, s * ge, lr, delta, wd); });
+}
+
 // ------------------------------------------------- local response norm
 //
 // Across channels, Caffe's form: s = k + alpha/size * (sum of x^2 over the
@@ -1028,6 +1044,22 @@ hipError_t launch_sgd(size_t n, float* w, const float* g, float* v, uint16_t* wb
   const unsigned grid = grid_for(n / 4 / UPD_U + 1, 256, 1u << 30);
   TraceScope ts("sgd_kernel", st, (double)n * (20.0 + (wb ? 2.0 : 0.0)), WORK_BYTE);
   hipLaunchKernelGGL(sgd_kernel, dim3(grid), dim3(256), 0, st, n, w, g, v, wb, lr, mom, wd);
+  return hipGetLastError();
+}
+
+hipError_t launch_sgd_scaled(size_t n, float* w, const float* g, float* v, uint16_t* wb, float lr, float mom, float wd,
+                             const float* scale, hipStream_t st) {
+  const unsigned grid = grid_for(n / 4 / UPD_U + 1, 256, 1u << 30);
+  TraceScope ts("sgd_scaled_kernel", st, (double)n * (20.0 + (wb ? 2.0 : 0.0)), WORK_BYTE);
+  hipLaunchKernelGGL(sgd_scaled_kernel, dim3(grid), dim3(256), 0, st, n, w, g, v, wb, lr, mom, wd, scale);
+  return hipGetLastError();
+}
+
+hipError_t launch_adagrad_scaled(size_t n, float* w, const float* g, float* h, uint16_t* wb, float lr, float delta, float wd,
+                                 const float* scale, hipStream_t st) {
+  const unsigned grid = grid_for(n / 4 / UPD_U + 1, 256, 1u << 30);
+  TraceScope ts("adagrad_scaled_kernel", st, (double)n * (20.0 + (wb ? 2.0 : 0.0)), WORK_BYTE);
+  hipLaunchKernelGGL(adagrad_scaled_kernel, dim3(grid), dim3(256), 0, st, n, w, g, h, wb, lr, delta, wd, scale);
   return hipGetLastError();
 }
 

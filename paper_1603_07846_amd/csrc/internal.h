@@ -207,5 +207,10 @@ hipError_t launch_adagrad(size_t n, float* w, const float* g, float* h, uint16_t
                           float wd, hipStream_t st);
 hipError_t launch_sgd(size_t n, float* w, const float* g, float* v, uint16_t* wb, float lr, float mom, float wd,
                       hipStream_t st);
+// The same with g multiplied by scale[0] (device memory).
+hipError_t launch_adagrad_scaled(size_t n, float* w, const float* g, float* h, uint16_t* wb, float lr, float delta,
+                                 float wd, const float* scale, hipStream_t st);
+hipError_t launch_sgd_scaled(size_t n, float* w, const float* g, float* v, uint16_t* wb, float lr, float mom, float wd,
+                             const float* scale, hipStream_t st);
 
 }  // namespace singa

@@ -41,6 +41,14 @@ EXPORTS = ["singa_strerror", "singa_conv_out_shape", "singa_pool_out_shape", "si
            "singa_trace_enable", "singa_trace_count", "singa_trace_get"]
 
 
+# every exported symbol of include/singa_mi_dense.h
+DENSE_EXPORTS = ["singa_linear_fwd_workspace_bytes", "singa_linear_fwd", "singa_linear_bwd_workspace_bytes",
+                 "singa_linear_bwd", "singa_linear_softmax_ce_workspace_bytes", "singa_linear_softmax_ce",
+                 "singa_grad_norm_workspace_bytes", "singa_grad_norm", "singa_grad_clip",
+                 "singa_sgd_momentum_update_scaled", "singa_adagrad_update_scaled"]
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+
+
 class LrnDesc(ctypes.Structure):
     _fields_ = [("size", ctypes.c_int), ("alpha", ctypes.c_float), ("beta", ctypes.c_float), ("k", ctypes.c_float)]
 
@@ -113,13 +121,27 @@ def _lib():
         lib.singa_trace_count.argtypes = []
         lib.singa_trace_get.argtypes = [i32, ctypes.POINTER(ctypes.c_char_p), ctypes.POINTER(ctypes.c_double),
                                         ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i32)]
-        for name in EXPORTS:
+        pi, pp, ps = ctypes.POINTER(i32), ctypes.POINTER(vp), ctypes.POINTER(sz)
+        lib.singa_linear_fwd_workspace_bytes.argtypes = [i32, i32, i32, i32, ps]
+        lib.singa_linear_fwd.argtypes = [i32, i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+        lib.singa_linear_bwd_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, ps]
+        lib.singa_linear_bwd.argtypes = [i32, i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp, i32, vp, sz, vp]
+        lib.singa_linear_softmax_ce_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, ps]
+        lib.singa_linear_softmax_ce.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, f32, vp, vp, vp, i32, vp, i32, vp,
+                                                sz, vp]
+        lib.singa_grad_norm_workspace_bytes.argtypes = [i32]
+        lib.singa_grad_norm.argtypes = [i32, pi, pp, ps, f32, vp, vp, sz, vp]
+        lib.singa_grad_clip.argtypes = [i32, pi, pp, pp, ps, f32, vp, vp, sz, vp]
+        lib.singa_sgd_momentum_update_scaled.argtypes = [sz, vp, vp, vp, vp, f32, f32, f32, vp, vp]
+        lib.singa_adagrad_update_scaled.argtypes = [sz, vp, vp, vp, vp, f32, f32, f32, vp, vp]
+        for name in EXPORTS + DENSE_EXPORTS:
             fn = getattr(lib, name)
             # pointers go in as Python integers, which ctypes would cut to 32
             # bits in a call without declared arguments
             assert fn.argtypes is not None, name
             if name != "singa_strerror":
                 fn.restype = i32
+        lib.singa_grad_norm_workspace_bytes.restype = sz
         _LIB = lib
     return _LIB
 
@@ -471,8 +493,14 @@ def softmax_ce(z, labels, loss=None, dz=None):
     return loss, dz
 
 
-def sgd_momentum_update(w, g, v, w_bf16=None, lr=0.01, momentum=0.9, weight_decay=0.0):
-    """Fused Updater step in place on fp32 w and v (and the bf16 shadow if given)."""
+def sgd_momentum_update(w, g, v, w_bf16=None, lr=0.01, momentum=0.9, weight_decay=0.0, grad_scale=None):
+    """Fused Updater step in place on fp32 w and v (and the bf16 shadow if given).
+    grad_scale: an fp32 device tensor of one value that multiplies g (grad_norm()[1:])."""
+    if grad_scale is not None:
+        _check("singa_sgd_momentum_update_scaled", _lib().singa_sgd_momentum_update_scaled(
+            w.numel(), _ptr(w), _ptr(g), _ptr(v), _ptr(w_bf16), float(lr), float(momentum), float(weight_decay),
+            _ptr(_factor(grad_scale)), _stream()))
+        return w, v
     _check("singa_sgd_momentum_update", _lib().singa_sgd_momentum_update(
         w.numel(), _ptr(w), _ptr(g), _ptr(v), _ptr(w_bf16), float(lr), float(momentum), float(weight_decay),
         _stream()))
@@ -502,12 +530,226 @@ def lrn_bwd(x, dy, size=5, alpha=1e-4, beta=0.75, k=1.0, layout="NHWC", out=None
     return dx
 
 
-def adagrad_update(w, g, h, w_bf16=None, lr=0.01, delta=1e-6, weight_decay=0.0):
-    """AdaGrad Updater step in place on fp32 w and h (and the bf16 shadow if given)."""
+def adagrad_update(w, g, h, w_bf16=None, lr=0.01, delta=1e-6, weight_decay=0.0, grad_scale=None):
+    """AdaGrad Updater step in place on fp32 w and h (and the bf16 shadow if given).
+    grad_scale: as for sgd_momentum_update."""
+    if grad_scale is not None:
+        _check("singa_adagrad_update_scaled", _lib().singa_adagrad_update_scaled(
+            w.numel(), _ptr(w), _ptr(g), _ptr(h), _ptr(w_bf16), float(lr), float(delta), float(weight_decay),
+            _ptr(_factor(grad_scale)), _stream()))
+        return w, h
     _check("singa_adagrad_update", _lib().singa_adagrad_update(
         w.numel(), _ptr(w), _ptr(g), _ptr(h), _ptr(w_bf16), float(lr), float(delta), float(weight_decay),
         _stream()))
     return w, h
+
+
+# ------------------------------------------------------------ dense layers
+def _dense(name, t, dtype, shape, current=None):
+    """t, if it is what the dense calls take: that dtype, that shape (None: any), contiguous, on the current device."""
+    if t.dtype != dtype:
+        raise TypeError("%s: %s wanted, got %s" % (name, dtype, t.dtype))
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError("%s: shape %s wanted, got %s" % (name, shape, tuple(t.shape)))
+    if not t.is_contiguous():
+        raise ValueError("%s: not contiguous" % name)
+    if not t.is_cuda or t.device.index != (_raw_device() if _raw_device is not None else torch.cuda.current_device()):
+        raise ValueError("%s: not on the current GPU (%s)" % (name, t.device))
+    return t
+
+
+def _factor(t):
+    return _dense("grad_scale", t, torch.float32, (1,))
+
+
+def _rows(x, w):
+    """(dtype code, rows, in, out) of x (..., in) and w (out, in)."""
+    dt = _dt(x)
+    if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1] or w.shape[0] < 1 or w.shape[1] < 1:
+        raise ValueError("x (..., in) and w (out, in) wanted, got %s and %s" % (tuple(x.shape), tuple(w.shape)))
+    _dense("x", x, x.dtype, None)
+    _dense("w", w, x.dtype, None)
+    return dt, x.numel() // w.shape[1], w.shape[1], w.shape[0]
+
+
+def _act(act) -> int:
+    if act not in ACTS:
+        raise ValueError("act: one of %s wanted, got %r" % (", ".join(ACTS), act))
+    return ACTS[act]
+
+
+def _dw_dt(x, dw_dtype) -> int:
+    if dw_dtype == torch.float32:
+        return F32
+    if dw_dtype == torch.bfloat16 and x.dtype == torch.bfloat16:
+        return BF16
+    raise TypeError("dw_dtype: torch.float32, or torch.bfloat16 with bf16 tensors, wanted, got %s" % dw_dtype)
+
+
+def _out(name, t, shape, dtype, device):
+    return empty(shape, dtype, device) if t is None else _dense(name, t, dtype, tuple(shape))
+
+
+def _dense_ws(nbytes, device, ws):
+    if ws is not None and nbytes:
+        _dense("workspace", ws, torch.uint8, None)
+    return _workspace(nbytes, device, ws)
+
+
+def _bytes(fn, *args) -> int:
+    out = ctypes.c_size_t(0)
+    _check(fn, getattr(_lib(), fn)(*args, ctypes.byref(out)))
+    return out.value
+
+
+@functools.lru_cache(maxsize=1024)
+def linear_fwd_workspace_bytes(dtype, rows, din, dout) -> int:
+    return _bytes("singa_linear_fwd_workspace_bytes", dtype if isinstance(dtype, int) else _dtype_code(dtype), rows, din,
+                  dout)
+
+
+@functools.lru_cache(maxsize=1024)
+def linear_bwd_workspace_bytes(dtype, rows, din, dout, act="none", dw_dtype=torch.float32) -> int:
+    return _bytes("singa_linear_bwd_workspace_bytes", dtype if isinstance(dtype, int) else _dtype_code(dtype), rows, din,
+                  dout, _act(act), _dtype_code(dw_dtype))
+
+
+@functools.lru_cache(maxsize=1024)
+def linear_softmax_ce_workspace_bytes(dtype, rows, din, classes, grad=True, dw_dtype=torch.float32) -> int:
+    return _bytes("singa_linear_softmax_ce_workspace_bytes", dtype if isinstance(dtype, int) else _dtype_code(dtype), rows,
+                  din, classes, int(bool(grad)), _dtype_code(dw_dtype))
+
+
+def _dtype_code(dtype) -> int:
+    if dtype == torch.float32:
+        return F32
+    if dtype == torch.bfloat16:
+        return BF16
+    raise TypeError("unsupported dtype %s" % dtype)
+
+
+def linear_fwd(x, w, bias=None, act="none", residual=None, keep_z=False, out=None, z=None, workspace=None):
+    """Inner product ComputeFeature: y = act(x w^T + bias) + residual, x (..., in), w (out, in), bias fp32.
+    keep_z (or z, a tensor for it): also the pre-activation x w^T + bias, which linear_bwd takes; then (y, z) is
+    returned.  act: "none", "relu", "gelu" (erf) or "silu"."""
+    dt, rows, din, dout = _rows(x, w)
+    a = _act(act)
+    shape = tuple(x.shape[:-1]) + (dout,)
+    if bias is not None:
+        _dense("bias", bias, torch.float32, (dout,))
+    if residual is not None:
+        _dense("residual", residual, x.dtype, shape)
+    y = _out("out", out, shape, x.dtype, x.device)
+    if keep_z or z is not None:
+        z = _out("z", z, shape, x.dtype, x.device)
+    ws = _dense_ws(linear_fwd_workspace_bytes(dt, rows, din, dout), x.device, workspace)
+    _check("singa_linear_fwd", _lib().singa_linear_fwd(
+        dt, rows, din, dout, _ptr(x), _ptr(w), _ptr(bias), a, _ptr(residual), _ptr(z), _ptr(y), _ptr(ws),
+        0 if ws is None else ws.numel(), _stream()))
+    return y if z is None else (y, z)
+
+
+def linear_bwd(x, w, dy, act="none", z=None, dx_residual=None, need_dx=True, need_dw=True, with_bias=True,
+               dw_dtype=torch.float32, dx=None, dw=None, db=None, accumulate=False, workspace=None):
+    """Inner product ComputeGradient: (dx, dw, db) (None where not asked for) from dy, the gradient at the output,
+    and the z that linear_fwd kept (not with act "none").  dx_residual: a gradient that reaches x another way,
+    added to dx.  dw is fp32, or bf16 with dw_dtype; accumulate adds into the given dw (fp32) and db."""
+    dt, rows, din, dout = _rows(x, w)
+    a, gt = _act(act), _dw_dt(x, dw_dtype)
+    shape = tuple(x.shape[:-1]) + (dout,)
+    _dense("dy", dy, x.dtype, shape)
+    if act == "none":
+        z = None
+    elif z is None:
+        raise ValueError("z: the kept pre-activation is wanted with act %r" % act)
+    else:
+        _dense("z", z, x.dtype, shape)
+    if dx_residual is not None:
+        _dense("dx_residual", dx_residual, x.dtype, tuple(x.shape))
+    if accumulate and ((need_dw and dw is None) or (with_bias and db is None)):
+        raise ValueError("accumulate: the dw and db to add into are wanted")
+    dx = _out("dx", dx, tuple(x.shape), x.dtype, x.device) if need_dx else None
+    dw = _out("dw", dw, (dout, din), dw_dtype, x.device) if need_dw else None
+    db = _out("db", db, (dout,), torch.float32, x.device) if with_bias else None
+    ws = _dense_ws(linear_bwd_workspace_bytes(dt, rows, din, dout, act, dw_dtype), x.device, workspace)
+    _check("singa_linear_bwd", _lib().singa_linear_bwd(
+        dt, rows, din, dout, _ptr(x), _ptr(w), _ptr(z), a, _ptr(dy), _ptr(dx_residual), _ptr(dx), _ptr(dw), gt,
+        _ptr(db), int(bool(accumulate)), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+    return dx, dw, db
+
+
+def linear_softmax_ce(x, w, labels, bias=None, grad=True, need_dx=True, need_dw=True, scale=1.0,
+                      dw_dtype=torch.float32, loss=None, dx=None, dw=None, db=None, accumulate=False, workspace=None):
+    """Softmax cross-entropy of x w^T + bias, x (..., in), w (classes, in), without keeping the logits: (loss, dx,
+    dw, db) with loss as in softmax_ce (the mean over the counted rows, then each row's) and, with grad, the
+    gradients of scale * loss (db when there is a bias).  A row whose label (int32, one per row) is outside
+    [0, classes) is padding: not counted, loss and gradient zero.  dw_dtype, accumulate: as in linear_bwd."""
+    dt, rows, din, classes = _rows(x, w)
+    gt = _dw_dt(x, dw_dtype)
+    _dense("labels", labels, torch.int32, tuple(x.shape[:-1]))
+    if bias is not None:
+        _dense("bias", bias, torch.float32, (classes,))
+    need_dx, need_dw, need_db = grad and need_dx, grad and need_dw, grad and bias is not None
+    if accumulate and ((need_dw and dw is None) or (need_db and db is None)):
+        raise ValueError("accumulate: the dw and db to add into are wanted")
+    loss = _out("loss", loss, (rows + 1,), torch.float32, x.device)
+    dx = _out("dx", dx, tuple(x.shape), x.dtype, x.device) if need_dx else None
+    dw = _out("dw", dw, (classes, din), dw_dtype, x.device) if need_dw else None
+    db = _out("db", db, (classes,), torch.float32, x.device) if need_db else None
+    any_grad = bool(need_dx or need_dw or need_db)
+    ws = _dense_ws(linear_softmax_ce_workspace_bytes(dt, rows, din, classes, any_grad, dw_dtype), x.device, workspace)
+    _check("singa_linear_softmax_ce", _lib().singa_linear_softmax_ce(
+        dt, rows, din, classes, _ptr(x), _ptr(w), _ptr(bias), _ptr(labels), float(scale), _ptr(loss), _ptr(dx), _ptr(dw),
+        gt, _ptr(db), int(bool(accumulate)), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+    return loss, dx, dw, db
+
+
+def _grad_list(tensors, name):
+    for t in tensors:
+        if not t.is_contiguous() or not t.is_cuda:
+            raise ValueError("%s: contiguous tensors on the current GPU wanted" % name)
+    if tensors:
+        _dense(name, tensors[0], tensors[0].dtype, None)
+        if any(t.device != tensors[0].device for t in tensors):
+            raise ValueError("%s: tensors on one GPU wanted" % name)
+    n = len(tensors)
+    return (ctypes.c_void_p * n)(*[t.data_ptr() for t in tensors])
+
+
+def _grad_stat(grads, max_norm, out, stat, workspace):
+    grads = list(grads)
+    n = len(grads)
+    if not n:
+        raise ValueError("grads: at least one tensor wanted")
+    ptrs = _grad_list(grads, "grads")
+    dtypes = (ctypes.c_int * n)(*[_dtype_code(t.dtype) for t in grads])
+    sizes = (ctypes.c_size_t * n)(*[t.numel() for t in grads])
+    device = grads[0].device
+    stat = _out("stat", stat, (2,), torch.float32, device)
+    ws = _dense_ws(_lib().singa_grad_norm_workspace_bytes(n), device, workspace)
+    if out is None:
+        _check("singa_grad_norm", _lib().singa_grad_norm(n, dtypes, ptrs, sizes, float(max_norm), _ptr(stat), _ptr(ws),
+                                                         ws.numel(), _stream()))
+        return stat
+    out = list(out)
+    if len(out) != n or any(o.shape != g.shape or o.dtype != g.dtype for o, g in zip(out, grads)):
+        raise ValueError("out: tensors of the gradients' shapes and types wanted")
+    _check("singa_grad_clip", _lib().singa_grad_clip(n, dtypes, ptrs, _grad_list(out, "out"), sizes, float(max_norm),
+                                                     _ptr(stat), _ptr(ws), ws.numel(), _stream()))
+    return stat
+
+
+def grad_norm(grads, max_norm=float("inf"), stat=None, workspace=None):
+    """The global norm over all gradient tensors (fp32 and bf16, mixed) and the factor that clips it to max_norm: an
+    fp32 device tensor (norm, scale), scale = max_norm / norm where norm > max_norm and is finite, else 1.  The
+    updates take stat[1:] as grad_scale."""
+    return _grad_stat(grads, max_norm, None, stat, workspace)
+
+
+def clip_grads(grads, max_norm, out=None, stat=None, workspace=None):
+    """grad_norm, then out[i] = scale * grads[i] (in place without out).  Returns (norm, scale) as grad_norm."""
+    grads = list(grads)
+    return _grad_stat(grads, max_norm, grads if out is None else out, stat, workspace)
 
 
 def trace_enable(on: bool = True):
