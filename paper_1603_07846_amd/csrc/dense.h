@@ -73,6 +73,7 @@ struct Product {
   int kb = 0;  // k rows that B has (0: K)
   int epi = EPI_OUT;
   Epilogue e;
+  bool raw = false;  // see product_splits
   const char* name = "";
   double flops = 0;
 };
@@ -88,6 +89,9 @@ constexpr int K_TILE = 64;  // a multiple of every kernel's K-tile
 // Workspace for the partial sums of a product whose tiles cannot fill the GPU.
 size_t product_partial_bytes(int dt, int M, int N, int K, int epi);
 hipError_t launch_product(const Product& p, float* partial, hipStream_t st);
+// Number of partial sums of that product; launch_product with `raw` writes
+// them ([M][N rounded up to 8] each, also when it is one) and stops there.
+int product_splits(int dt, int M, int N, int K);
 
 // The same product for few rows (M <= SKINNY_ROWS), A and B both K contiguous
 // with ld = K, any alignment: a pass over B.  EPI_OUT and EPI_LSE (STAT_COLS
@@ -118,14 +122,42 @@ hipError_t launch_lse(const float2* stats, int nstat, const float* zlab, const i
 // loss[0] = mean of loss[1 ..] over the counted rows, unit = scale / count (0 when none; may be null)
 hipError_t launch_loss_mean(const int32_t* labels, int classes, long rows, float* loss, float* unit, float scale,
                             hipStream_t st);
-// Rows of kept logits z (fp32 [rows][ldz], the bias included): loss[1 + row]
-// and, unless null, dlogits dz as EPI_DLOGITS makes them (T [rows_padded][ldd],
-// zero past rows and classes), their further terms, and their unrounded values dzf (fp32
-// [rows][ldz], may be z).
-hipError_t launch_loss_rows(int dt, const float* z, long ldz, const int32_t* labels, long rows, long rows_padded,
-                            int classes, float* loss, void* dz, void* more, long ldd, float* dzf,
-                            hipStream_t st);
-// colsum [groups][cols] of dzf [rows][ld] over COLSUM_ROWS rows each
-hipError_t launch_colsum_rows(const float* dzf, long ld, float* colsum, long rows, int cols, hipStream_t st);
+// The same two at once, for few rows (a workgroup goes through them).
+constexpr int LSE_FINISH_ROWS = 4;
+hipError_t launch_lse_finish(const float2* stats, int nstat, const float* zlab, const int32_t* labels, int classes, int rows,
+                             float* loss, hipStream_t st);
+// Rows of kept logits: z holds `splits` partial sums [rows][ldz] of them (the
+// bias not added).  Written: loss[1 + row]; unless dz is null the dlogits as
+// EPI_DLOGITS makes them (T [rows_padded][ldd], zero past rows and classes)
+// and their further terms (more); with keep_dz their unrounded values into
+// the first [rows][ldz] of z (rows with a valid label only); unless xc is null
+// the rows of x as launch_pack makes them with labels.
+struct LossRows {
+  float* z;
+  long ldz;
+  int splits;
+  const float* bias;
+  const int32_t* labels;
+  long rows, rows_padded;
+  int classes;
+  float* loss;
+  void *dz, *more;
+  long ldd;
+  int keep_dz;
+  const void* x;
+  void* xc;
+  int in;
+  long ldx;
+};
+hipError_t launch_loss_rows(int dt, const LossRows& a, hipStream_t st);
+// The mean and the unit (may be null) of up to FINISH_ROWS rows and, unless db
+// is null, db (+)= unit times the sum of the valid rows of dz.
+constexpr int FINISH_ROWS = 1024;
+hipError_t launch_loss_finish(const int32_t* labels, int classes, int rows, float* loss, float* unit, float scale,
+                              const float* dz, long ld, float* db, int add, hipStream_t st);
+// colsum [groups][cols] of dzf [rows][ld] over COLSUM_ROWS rows each, those
+// with a valid label
+hipError_t launch_colsum_rows(const float* dzf, long ld, float* colsum, long rows, int cols, const int32_t* labels,
+                              int classes, hipStream_t st);
 
 }  // namespace singa

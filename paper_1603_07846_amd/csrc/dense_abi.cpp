@@ -123,8 +123,8 @@ struct LossWs {
   Packed k;
   bool keep, skinny, split, one;  // logits kept; few rows; dlogits in TERMS terms; one piece
   long ldd, rows_padded, piece;   // dlogits: row length, rows; classes per piece
-  int nstat;
-  long ldl;  // row length of kept logits
+  int nstat, splits;  // splits, ldl: partial sums of kept logits and their row length
+  long ldl;
   void *dz, *more, *xc, *xp, *wp;
   float *unit, *lse, *zlab, *logits, *dxf, *colsum, *partial;
   float2* stats;
@@ -147,8 +147,8 @@ size_t carve_loss(int dt, int rows, int in, int classes, bool grad, int dw_dt, v
   o->xp = c.take(tiles && o->k.copy ? (size_t)rows * o->k.ld * es : 0);
   size_t partial = 0;
   if (o->keep) {
-    o->logits = c.take<float>((size_t)rows * o->ldl);
-    if (!o->skinny) partial = product_partial_bytes(dt, rows, classes, in, EPI_OUT);
+    o->splits = o->skinny ? 1 : product_splits(dt, rows, classes, in);
+    o->logits = c.take<float>((size_t)o->splits * rows * o->ldl);
   } else {
     o->nstat = (classes + (o->skinny ? SKINNY_COLS : STAT_COLS) - 1) / (o->skinny ? SKINNY_COLS : STAT_COLS);
     o->stats = c.take<float2>((size_t)rows * o->nstat);
@@ -389,19 +389,46 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
   const bool split = o.split && dw;
   void* more = split ? o.more : nullptr;
   const long groups = up(rows, COLSUM_ROWS) / COLSUM_ROWS;
+  const bool finish = o.keep && rows <= FINISH_ROWS;  // the mean and db in one kernel
   if (o.keep) {
     // the logits, then their rows
-    p.e.labels = nullptr;
-    p.e.y = o.logits;
-    p.e.ldy = o.ldl;
-    p.e.out_f32 = 1;
+    Product q = p;
+    q.e = Epilogue{};
+    q.e.y = o.logits;  // few rows' kernel
+    q.e.ldy = o.ldl;
+    q.e.out_f32 = 1;
+    q.raw = true;
     if (e == hipSuccess) {
-      p.name = o.skinny ? "skinny_kernel" : "product_kernel<logits>";
-      e = o.skinny ? launch_skinny(p, st) : launch_product(p, o.partial, st);
+      q.name = o.skinny ? "skinny_kernel" : "product_kernel<logits>";
+      e = o.skinny ? launch_skinny(q, st) : launch_product(q, o.logits, st);
     }
-    if (e == hipSuccess)
-      e = launch_loss_rows(dtype, o.logits, o.ldl, labels, rows, o.rows_padded, classes, loss, grad ? o.dz : nullptr, more,
-                           o.ldd, db ? o.logits : nullptr, st);
+    LossRows r{};
+    r.z = o.logits;
+    r.ldz = o.ldl;
+    r.splits = o.splits;
+    r.bias = bias;
+    r.labels = labels;
+    r.rows = rows;
+    r.rows_padded = o.rows_padded;
+    r.classes = classes;
+    r.loss = loss;
+    if (!grad) {
+      r.rows_padded = rows;
+    } else {
+      r.dz = o.dz;
+      r.more = more;
+      r.ldd = o.ldd;
+      r.keep_dz = db != nullptr;
+    }
+    if (dw) {
+      r.x = x;
+      r.xc = o.xc;
+      r.in = in;
+      r.ldx = o.k.ld;
+    }
+    if (e == hipSuccess) e = launch_loss_rows(dtype, r, st);
+    if (e == hipSuccess && finish)
+      e = launch_loss_finish(labels, classes, rows, loss, grad ? o.unit : nullptr, scale, o.logits, o.ldl, db, accumulate, st);
   } else {
     p.epi = EPI_LSE;
     p.e.stats = o.stats;
@@ -411,14 +438,16 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
       p.name = o.skinny ? "skinny_kernel" : "product_kernel<lse>";
       e = o.skinny ? launch_skinny(p, st) : launch_product(p, nullptr, st);
     }
+    if (!grad && rows <= LSE_FINISH_ROWS)
+      return status(e == hipSuccess ? launch_lse_finish(o.stats, o.nstat, o.zlab, labels, classes, rows, loss, st) : e);
     if (e == hipSuccess) e = launch_lse(o.stats, o.nstat, o.zlab, labels, classes, rows, o.lse, loss, st);
   }
-  if (e == hipSuccess) e = launch_loss_mean(labels, classes, rows, loss, grad ? o.unit : nullptr, scale, st);
+  if (e == hipSuccess && !finish) e = launch_loss_mean(labels, classes, rows, loss, grad ? o.unit : nullptr, scale, st);
   if (!grad || e != hipSuccess) return status(e);
 
   // x without its padding rows, for dw: a zero gradient times what they hold
   // need not be zero
-  if (dw) e = launch_pack(dtype, x, o.xc, rows, in, o.k.ld, labels, classes, st);
+  if (dw && !o.keep) e = launch_pack(dtype, x, o.xc, rows, in, o.k.ld, labels, classes, st);
   const long es = (long)dt_size(dtype);
   for (long c0 = 0; c0 < classes && e == hipSuccess; c0 += o.piece) {
     const int n = (int)std::min(o.piece, classes - c0);
@@ -440,10 +469,10 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
       q.e.rows_padded = (int)o.rows_padded;
       q.e.colsum = db ? o.colsum : nullptr;
       e = launch_product(q, nullptr, st);
-    } else if (db) {
-      e = launch_colsum_rows(o.logits, o.ldl, o.colsum, rows, classes, st);
+    } else if (db && !finish) {
+      e = launch_colsum_rows(o.logits, o.ldl, o.colsum, rows, classes, labels, classes, st);
     }
-    if (e == hipSuccess && db) e = launch_colsum(o.colsum, db + c0, groups, n, accumulate, o.unit, st);
+    if (e == hipSuccess && db && !finish) e = launch_colsum(o.colsum, db + c0, groups, n, accumulate, o.unit, st);
     if (e == hipSuccess && dx) {
       Product q;
       q.name = "product_kernel<bwd_data>";

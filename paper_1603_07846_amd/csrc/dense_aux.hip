@@ -238,14 +238,16 @@ __global__ __launch_bounds__(256) void dact_kernel(int act, const T* __restrict_
 }
 
 __global__ __launch_bounds__(256) void colsum_rows_kernel(const float* __restrict__ in, long ld, float* __restrict__ colsum,
-                                                          long rows, int cols) {
+                                                          long rows, int cols, const int32_t* __restrict__ labels,
+                                                          int classes) {
   __shared__ float red[4][64];
   const int tc = threadIdx.x & 63, tr = threadIdx.x >> 6;
   const int col = blockIdx.y * 64 + tc;
   const long row0 = (long)blockIdx.x * COLSUM_ROWS;
   float s = 0.f;
   if (col < cols)
-    for (int i = tr; i < COLSUM_ROWS && row0 + i < rows; i += 4) s += in[(row0 + i) * ld + col];
+    for (int i = tr; i < COLSUM_ROWS && row0 + i < rows; i += 4)
+      s += label_ok(labels[row0 + i], classes) ? in[(row0 + i) * ld + col] : 0.f;
   red[tr][tc] = s;
   __syncthreads();
   if (tr == 0 && col < cols) colsum[(long)blockIdx.x * cols + col] = red[0][tc] + red[1][tc] + red[2][tc] + red[3][tc];
@@ -289,7 +291,7 @@ __device__ __forceinline__ void merge(float& m, float& s, float m2, float s2) {
   m = mx;
 }
 
-// Over W threads (a wave, or a whole workgroup of 256) that each hold a set.
+// Over W threads (a wave, or a whole workgroup) that each hold a set.
 template <int W> __device__ __forceinline__ void merge_all(float& m, float& s, float2* lds) {
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
@@ -354,44 +356,149 @@ __global__ __launch_bounds__(1024) void loss_mean_kernel(const int32_t* __restri
   if (unit) unit[0] = n > 0 ? (float)(scale / n) : 0.f;
 }
 
-// W threads per row of kept logits; dzf may be z itself.
+// W threads per row of kept logits, given as the partial sums of their product
+// (S of them, without the bias).  The first pass adds them up, leaves the logit
+// in the first one's place and takes the maximum and sum as it goes; the second
+// reads the logits back (from the thread's own stores) and leaves the unrounded
+// dlogits there for the column sums.  The row of x goes along, cleaned.
 template <typename T, int W>
-__global__ __launch_bounds__(256) void loss_rows_kernel(const float* z, long ldz, const int32_t* __restrict__ labels,
-                                                        long rows, long rows_padded, int classes,
-                                                        float* __restrict__ loss, T* __restrict__ dz, bf16_t* __restrict__ more,
-                                                        long ldd, float* dzf) {
+__global__ __launch_bounds__(256) void loss_rows_kernel(LossRows a) {
   __shared__ float2 lds[4];
-  const int t = threadIdx.x % W;
-  const long row = (long)blockIdx.x * (256 / W) + threadIdx.x / W;
-  if (row >= rows_padded) return;
-  const int lab = row < rows ? labels[row] : -1;
-  const bool live = label_ok(lab, classes);
-  const float* zr = z + (size_t)(row < rows ? row : 0) * ldz;
+  __shared__ float zl[4];
+  const int t = threadIdx.x % W, in_wg = threadIdx.x / W;
+  const long row = (long)blockIdx.x * (256 / W) + in_wg;
+  if (row >= a.rows_padded) return;
+  const int lab = row < a.rows ? a.labels[row] : -1;
+  const bool live = label_ok(lab, a.classes);
+  if (a.xc && row < a.rows) {
+    constexpr int VEC = TypeInfo<T>::VEC;
+    const T* xr = (const T*)a.x + row * a.in;
+    T* o = (T*)a.xc + row * a.ldx;
+    for (int c = t * VEC; c < a.ldx; c += W * VEC) {
+      union { uint4 u; T e[VEC]; } v;
+      v.u = make_uint4(0, 0, 0, 0);
+      if (live) {
+        if (a.in % VEC == 0) {
+          v.u = *(const uint4*)(xr + c);
+        } else {
+#pragma unroll
+          for (int j = 0; j < VEC; ++j)
+            if (c + j < a.in) v.e[j] = xr[c + j];
+        }
+      }
+      *(uint4*)(o + c) = v.u;
+    }
+  }
+  float* zr = a.z + (size_t)(row < a.rows ? row : 0) * a.ldz;
+  const size_t step = (size_t)a.rows * a.ldz;
   float lse = 0.f;
   if (live) {  // the same for all threads of a row
     float m = -INFINITY, s = 0.f;
-    for (int c = t; c < classes; c += W) m = fmaxf(m, zr[c]);
-    const float base = m == -INFINITY ? 0.f : m;
-    for (int c = t; c < classes; c += W) s += exp_fast(zr[c] - base);
+    constexpr int U = 4;
+    for (int c0 = t; c0 < a.classes; c0 += U * W) {
+      float v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = c0 + u * W < a.classes ? zr[c0 + u * W] : -INFINITY;
+      for (int p = 1; p < a.splits; ++p) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] += c0 + u * W < a.classes ? zr[p * step + c0 + u * W] : 0.f;
+      }
+      float mx = m;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + u * W;
+        if (c < a.classes) {
+          if (a.bias) v[u] += a.bias[c];
+          zr[c] = v[u];
+          if (c == lab) zl[in_wg] = v[u];
+        }
+        mx = fmaxf(mx, v[u]);
+      }
+      const float base = mx == -INFINITY ? 0.f : mx;
+      s *= exp_fast(m - base);
+#pragma unroll
+      for (int u = 0; u < U; ++u) s += exp_fast(v[u] - base);
+      m = mx;
+    }
     merge_all<W>(m, s, lds);
     lse = m + logf(s);
   }
-  if (t == 0 && row < rows) loss[1 + row] = live ? lse - zr[lab] : 0.f;
-  if (!dz) return;
-  if constexpr (W > 64) __syncthreads();  // the label's logit is read before dzf overwrites it
-  for (long c = t; c < ldd; c += W) {
+  if constexpr (W > 64) __syncthreads();  // the label's logit
+  __builtin_amdgcn_wave_barrier();
+  if (t == 0 && row < a.rows) a.loss[1 + row] = live ? lse - zl[in_wg] : 0.f;
+  if (!a.dz) return;
+  for (long c = t; c < a.ldd; c += W) {
     float v = 0.f;
-    if (live && c < classes) v = exp_fast(zr[c] - lse) - (c == lab ? 1.f : 0.f);
-    store_out<T>(dz + row * ldd + c, v);
-    if (sizeof(T) == 2 && more) {
+    if (live && c < a.classes) v = exp_fast(zr[c] - lse) - (c == lab ? 1.f : 0.f);
+    store_out<T>((T*)a.dz + row * a.ldd + c, v);
+    if (sizeof(T) == 2 && a.more) {
       float left = v;
       for (int i = 0; i < TERMS - 1; ++i) {
         left -= bf16_to_f32(f32_to_bf16(left));
-        more[(i * rows_padded + row) * ldd + c] = f32_to_bf16(left);
+        ((bf16_t*)a.more)[(i * a.rows_padded + row) * a.ldd + c] = f32_to_bf16(left);
       }
     }
-    if (dzf && row < rows && c < classes) dzf[row * ldz + c] = v;
+    if (a.keep_dz && row < a.rows && c < a.classes) zr[c] = v;
   }
+}
+
+// For up to FINISH_ROWS rows: the mean, and the bias gradient from the
+// unrounded dlogits, 32 columns a workgroup.  Each workgroup counts the rows
+// for itself; the first one writes the mean and the unit.
+__global__ __launch_bounds__(1024) void loss_finish_kernel(const int32_t* __restrict__ labels, int classes, int rows,
+                                                           float* __restrict__ loss, float* __restrict__ unit, float scale,
+                                                           const float* __restrict__ dz, long ld, float* __restrict__ db,
+                                                           int add) {
+  __shared__ double lds[16];
+  __shared__ float red[32][33];
+  const int t = threadIdx.x;
+  const bool ok = t < rows && label_ok(labels[t], classes);
+  const double n = block_sum(ok ? 1.0 : 0.0, lds);
+  const float un = n > 0 ? (float)(scale / n) : 0.f;
+  if (blockIdx.x == 0) {
+    const double s = block_sum(ok ? (double)loss[1 + t] : 0.0, lds);
+    if (t == 0) {
+      loss[0] = n > 0 ? (float)(s / n) : 0.f;
+      if (unit) unit[0] = un;
+    }
+  }
+  if (!db) return;
+  const int tc = t & 31, tr = t >> 5, col = blockIdx.x * 32 + tc;
+  float s = 0.f;
+  if (col < classes)
+    for (int r = tr; r < rows; r += 32) s += label_ok(labels[r], classes) ? dz[(size_t)r * ld + col] : 0.f;
+  red[tr][tc] = s;
+  __syncthreads();
+  if (tr || col >= classes) return;
+  s = 0.f;
+#pragma unroll
+  for (int r = 0; r < 32; ++r) s += red[r][tc];
+  s *= un;
+  db[col] = add ? db[col] + s : s;
+}
+
+// One or a few rows of many column groups: the loss of each, and the mean.
+__global__ __launch_bounds__(1024) void lse_finish_kernel(const float2* __restrict__ stats, int nstat,
+                                                          const float* __restrict__ zlab, const int32_t* __restrict__ labels,
+                                                          int classes, int rows, float* __restrict__ loss) {
+  __shared__ float2 lds[16];
+  double sum = 0;
+  int n = 0;
+  for (int row = 0; row < rows; ++row) {
+    float m = -INFINITY, s = 0.f;
+    for (int i = threadIdx.x; i < nstat; i += 1024) {
+      const float2 p = stats[(size_t)row * nstat + i];
+      merge(m, s, p.x, p.y);
+    }
+    merge_all<1024>(m, s, lds);
+    __syncthreads();
+    const bool ok = label_ok(labels[row], classes);
+    const float l = ok ? m + logf(s) - zlab[row] : 0.f;
+    if (threadIdx.x == 0) loss[1 + row] = l;
+    sum += l;
+    n += ok;
+  }
+  if (threadIdx.x == 0) loss[0] = n ? (float)(sum / n) : 0.f;
 }
 
 }  // namespace
@@ -438,10 +545,11 @@ hipError_t launch_colsum(const float* colsum, float* out, long groups, int cols,
   return hipGetLastError();
 }
 
-hipError_t launch_colsum_rows(const float* dzf, long ld, float* colsum, long rows, int cols, hipStream_t st) {
+hipError_t launch_colsum_rows(const float* dzf, long ld, float* colsum, long rows, int cols, const int32_t* labels,
+                              int classes, hipStream_t st) {
   TraceScope ts("colsum_rows_kernel", st, 4.0 * rows * cols, WORK_BYTE);
   const dim3 grid((unsigned)((rows + COLSUM_ROWS - 1) / COLSUM_ROWS), (unsigned)((cols + 63) / 64));
-  hipLaunchKernelGGL(colsum_rows_kernel, grid, dim3(256), 0, st, dzf, ld, colsum, rows, cols);
+  hipLaunchKernelGGL(colsum_rows_kernel, grid, dim3(256), 0, st, dzf, ld, colsum, rows, cols, labels, classes);
   return hipGetLastError();
 }
 
@@ -476,22 +584,36 @@ hipError_t launch_loss_mean(const int32_t* labels, int classes, long rows, float
   return hipGetLastError();
 }
 
-hipError_t launch_loss_rows(int dt, const float* z, long ldz, const int32_t* labels, long rows, long rows_padded, int classes,
-                            float* loss, void* dz, void* more, long ldd, float* dzf, hipStream_t st) {
-  TraceScope ts("loss_rows_kernel", st, (double)rows * classes * (8 + dt_size(dt)), WORK_BYTE);
-  const bool wide = classes > 1024;  // a workgroup per row, else a wave
-  const dim3 grid((unsigned)(wide ? rows_padded : (rows_padded + 3) / 4));
-#define SINGA_ROWS(T, W)                                                                                                     \
-  hipLaunchKernelGGL((loss_rows_kernel<T, W>), grid, dim3(256), 0, st, z, ldz, labels, rows, rows_padded, classes, loss, \
-                     (T*)dz, (bf16_t*)more, ldd, dzf)
+hipError_t launch_loss_rows(int dt, const LossRows& a, hipStream_t st) {
+  TraceScope ts("loss_rows_kernel", st, (double)a.rows * a.classes * (8 + dt_size(dt)), WORK_BYTE);
+  const bool wide = a.classes > 256;  // a workgroup per row, else a wave
+  const dim3 grid((unsigned)(wide ? a.rows_padded : (a.rows_padded + 3) / 4));
   if (dt == BF16) {
-    if (wide) SINGA_ROWS(bf16_t, 256);
-    else SINGA_ROWS(bf16_t, 64);
+    if (wide)
+      hipLaunchKernelGGL((loss_rows_kernel<bf16_t, 256>), grid, dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL((loss_rows_kernel<bf16_t, 64>), grid, dim3(256), 0, st, a);
   } else {
-    if (wide) SINGA_ROWS(float, 256);
-    else SINGA_ROWS(float, 64);
+    if (wide)
+      hipLaunchKernelGGL((loss_rows_kernel<float, 256>), grid, dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL((loss_rows_kernel<float, 64>), grid, dim3(256), 0, st, a);
   }
-#undef SINGA_ROWS
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_finish(const int32_t* labels, int classes, int rows, float* loss, float* unit, float scale,
+                              const float* dz, long ld, float* db, int add, hipStream_t st) {
+  TraceScope ts("loss_finish_kernel", st, db ? 4.0 * rows * classes : 8.0 * rows, WORK_BYTE);
+  hipLaunchKernelGGL(loss_finish_kernel, dim3(db ? (unsigned)((classes + 31) / 32) : 1u), dim3(1024), 0, st, labels, classes,
+                     rows, loss, unit, scale, dz, ld, db, add);
+  return hipGetLastError();
+}
+
+hipError_t launch_lse_finish(const float2* stats, int nstat, const float* zlab, const int32_t* labels, int classes, int rows,
+                             float* loss, hipStream_t st) {
+  TraceScope ts("lse_finish_kernel", st, 8.0 * rows * nstat, WORK_BYTE);
+  hipLaunchKernelGGL(lse_finish_kernel, dim3(1), dim3(1024), 0, st, stats, nstat, zlab, labels, classes, rows, loss);
   return hipGetLastError();
 }
 

@@ -11,6 +11,8 @@ size_t product_partial_bytes(int dt, int M, int N, int K, int epi) {
   return p.splits > 1 ? (size_t)p.splits * M * (((size_t)N + 7) / 8 * 8) * 4 : 0;
 }
 
+int product_splits(int dt, int M, int N, int K) { return plan_product(dt, M, N, K, EPI_OUT).splits; }
+
 hipError_t launch_product(const Product& p, float* partial, hipStream_t st) {
   return p.dt == BF16 ? launch_product_bf16(p, partial, st) : launch_product_t<float>(p, partial, st);
 }

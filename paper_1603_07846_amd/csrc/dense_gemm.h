@@ -2,7 +2,7 @@
 //
 // A workgroup computes a BM x BN tile; the K range goes through LDS in tiles
 // of 128 bytes (64 bf16 or 32 fp32 values of k), written there straight from
-// memory (buffer loads to LDS) two stages deep.  An operand is staged the way
+// memory (buffer loads to LDS), two stages.  An operand is staged the way
 // it is stored:
 //   K contiguous:    BM rows of 128 bytes; a lane's fragment (8 bf16 or 4 fp32
 //                    of one row) is one 16-byte read.  16-byte chunk c of row
@@ -38,6 +38,7 @@ struct GemmArgs {
   int tiles_m, tiles_n;
   float* partial;           // [splits][M][ldp] when splits > 1
   long ldp;
+  int raw;                  // the sums as they are go to `partial`
   int vec;                  // outputs take 16-byte vectors
   Epilogue e;
 };
@@ -199,6 +200,8 @@ __device__ __forceinline__ void epi_out(const Epilogue& e, int N, bool vec, int 
   }
 }
 
+template <int V> struct Const { static constexpr int value = V; };
+
 template <typename T> struct TypeInfo;
 template <> struct TypeInfo<bf16_t> {
   static constexpr int VEC = 8, BK = 64;
@@ -230,37 +233,47 @@ template <typename T, bool KC, int R, int NW> struct Tile {
   static constexpr int CPR = RB / 16;
 
   uint32_t off[NI];  // within the tile's rsrc; OOB: nothing to read
-  int kch[NI];       // K contiguous: the chunk's k position within the K-tile
 
+  // K contiguous: the chunk of the K-tile that instruction i of this lane loads
+  __device__ __forceinline__ static int chunk(int wave, int lane, int i) {
+    return (lane & 7) ^ ((((wave * NI + i) * 8 + (lane >> 3)) >> 1) & 7);
+  }
   __device__ __forceinline__ void init(int wave, int lane, long ld, int r0, int rows) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int idx = wave * NI + i;
       if constexpr (KC) {
         const int r = idx * 8 + (lane >> 3);
-        kch[i] = (lane & 7) ^ ((r >> 1) & 7);
-        off[i] = r0 + r < rows ? (uint32_t)(r * ld + kch[i] * 16) : OOB;
+        off[i] = r0 + r < rows ? (uint32_t)(r * ld + chunk(wave, lane, i) * 16) : OOB;
       } else {
         constexpr int RPI = 1024 / RB;
         const int d = idx * RPI + lane / CPR;
         const int c = (lane % CPR) ^ (ES == 2 ? 4 * (d & 3) : 8 * ((d >> 2) & 1));
         off[i] = r0 + c * VEC < (rows + VEC - 1) / VEC * VEC ? (uint32_t)(d * ld + c * 16) : OOB;
-        kch[i] = d;
       }
     }
   }
+  // the last K-tile holds only kleft chunks of K
+  __device__ __forceinline__ void mask(int wave, int lane, int kleft) {
+    if constexpr (KC) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+        if (chunk(wave, lane, i) >= kleft) off[i] = OOB;
+    }
+  }
   // the rsrc of K-tile kt: the tile's corner, and the bytes from there to the
-  // operand's end
-  __device__ __forceinline__ static __amdgpu_buffer_rsrc_t rsrc(const char* p, long ld, long end, int r0, int kt) {
+  // operand's end; none where the K-tile is not wanted
+  __device__ __forceinline__ static __amdgpu_buffer_rsrc_t rsrc(const char* p, long ld, long end, int r0, int kt, bool live) {
     const long at = KC ? (long)r0 * ld + (long)kt * 128 : (long)kt * BK * ld + (long)r0 * ES;
     const long left = end - at;
-    const uint32_t n = left <= 0 ? 0u : left > 0x7ffffff0L ? 0x7ffffff0u : (uint32_t)left;
-    return make_rsrc(p + (left <= 0 ? 0 : at), n);
+    uint32_t n = left > 0x7ffffff0L ? 0x7ffffff0u : (uint32_t)left;
+    if (!live || left <= 0) n = 0;
+    return make_rsrc(p + at, n);
   }
-  // kleft: K contiguous: chunks of K from this K-tile on
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, char* lds, int wave, int i, int kleft) const {
-    const uint32_t o = KC ? (kch[i] < kleft ? off[i] : OOB) : off[i];
-    ld_lds16_asm(rs, o, lds + (wave * NI + i) * 1024);
+  // instruction i of this wave; lds: the LDS address of the wave's part
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, uint32_t lds, int i) const {
+    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + i * 1024), "v"(off[i]), "s"(rs)
+                 : "memory");
   }
 };
 
@@ -304,6 +317,13 @@ template <typename T, bool KC, int R, int F> struct Frags {
 };
 
 // WM x WN waves of (32 FM) x (32 FN).
+//
+// A K-tile is four steps of FM x FN matrix instructions (per 16 bytes of k).
+// Between the instructions of a step the wave reads the fragments of the next
+// one, so the matrix unit does not wait for LDS; the barrier of a K-tile comes
+// before its last step, whose instructions cover the first reads of the next
+// K-tile and the issue of the loads of the one after that, into the stage that
+// the barrier has freed.  Loads have a whole K-tile's time to land.
 template <typename T, bool AKC, bool BKC, int WM, int WN, int FM, int FN, int EPI>
 __global__ __launch_bounds__(WM* WN * 64) void product_kernel(GemmArgs g) {
   constexpr int NW = WM * WN, BM = WM * FM * 32, BN = WN * FN * 32;
@@ -345,39 +365,82 @@ __global__ __launch_bounds__(WM* WN * 64) void product_kernel(GemmArgs g) {
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
   const int kt0 = split * g.kt_split, kt1 = min(g.kt_all, kt0 + g.kt_split);
-  auto issue = [&](int kt, char* s) {
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem);
+  const uint32_t lds_a = lds0 + wave * TA::NI * 1024, lds_b = lds0 + TA::BYTES + wave * TB::NI * 1024;
+  __amdgpu_buffer_rsrc_t ra, rb;
+  // what loading K-tile kt takes
+  auto prepare = [&](int kt) {
     int kb = kt;  // the K-tile of B
     static_assert(TERMS == 3, "two places where B starts again");
     if (g.wrap && kb >= g.wrap) kb -= g.wrap;
     if (g.wrap && kb >= g.wrap) kb -= g.wrap;
-    const auto ra = TA::rsrc(g.a, g.lda, g.enda, m0, kt);
-    const auto rb = TB::rsrc(g.b, g.ldb, g.endb, n0, kb);
-#pragma unroll
-    for (int i = 0; i < TA::NI; ++i) ta.load(ra, s, wave, i, g.kca - kt * 8);
-#pragma unroll
-    for (int i = 0; i < TB::NI; ++i) tb.load(rb, s + TA::BYTES, wave, i, g.kcb - kb * 8);
-  };
-  if (kt0 < kt1) issue(kt0, smem);
-  int stage = 0;
-  for (int kt = kt0; kt < kt1; ++kt) {
-    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0): this K-tile has landed for this wave, its LDS reads are done
-    block_barrier();  // ... and for everyone, and everyone is done with the other stage
-    if (kt + 1 < kt1) issue(kt + 1, smem + (stage ^ 1) * STAGE);
-    const char* s = smem + stage * STAGE;
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      typename Chunk<T>::type af[FM], bf[FN];
-#pragma unroll
-      for (int b = 0; b < FM; ++b) af[b] = fa.read(s, b, ks);
-#pragma unroll
-      for (int b = 0; b < FN; ++b) bf[b] = fb.read(s + TA::BYTES, b, ks);
-#pragma unroll
-      for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) mma32(af[i], bf[j], acc[i][j]);
+    ra = TA::rsrc(g.a, g.lda, g.enda, m0, kt, kt < kt1);
+    rb = TB::rsrc(g.b, g.ldb, g.endb, n0, kb, kt < kt1);
+    if ((AKC || BKC) && kt == g.kt_all - 1) {
+      ta.mask(wave, lane, g.kca - kt * 8);
+      tb.mask(wave, lane, g.kcb - kb * 8);
     }
-    stage ^= 1;
+  };
+  constexpr int NL = TA::NI + TB::NI;
+  auto load = [&](int i, uint32_t stage) {
+    if (i < TA::NI)
+      ta.load(ra, lds_a + stage, i);
+    else
+      tb.load(rb, lds_b + stage, i - TA::NI);
+  };
+  typename Chunk<T>::type af[2][FM], bf[2][FN];
+  // the matrix instructions of one step on fragments `cur`, with the reads of
+  // step ks at s into the other set and, with LOADS, all loads in between
+  auto step = [&](auto cur_, const char* s, auto ks_, auto loads_, uint32_t stage) {
+    constexpr int cur = decltype(cur_)::value, nxt = cur ^ 1, ks = decltype(ks_)::value, N = FM * FN;
+    constexpr bool LOADS = decltype(loads_)::value;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      // fragments in the order in which the next step wants them
+#pragma unroll
+      for (int f = n * (FM + FN) / N; f < (n + 1) * (FM + FN) / N; ++f) {
+        if (f < FN)
+          bf[nxt][f] = fb.read(s + TA::BYTES, f, ks);
+        else
+          af[nxt][f - FN] = fa.read(s, f - FN, ks);
+      }
+      if constexpr (LOADS) {
+#pragma unroll
+        for (int l = n * NL / N; l < (n + 1) * NL / N; ++l) load(l, stage);
+      }
+      mma32(af[cur][n / FN], bf[cur][n % FN], acc[n / FN][n % FN]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  if (kt0 < kt1) {
+    prepare(kt0);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) load(i, 0);
+    prepare(kt0 + 1);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) load(i, STAGE);
+    wait_vmcnt<NL>();  // the first K-tile has landed for this wave
+    block_barrier();   // ... and for everyone
+#pragma unroll
+    for (int b = 0; b < FN; ++b) bf[0][b] = fb.read(smem + TA::BYTES, b, 0);
+#pragma unroll
+    for (int b = 0; b < FM; ++b) af[0][b] = fa.read(smem, b, 0);
+    uint32_t stage = 0;
+    for (int kt = kt0; kt < kt1; ++kt) {
+      const char* s = smem + stage;
+      step(Const<0>{}, s, Const<1>{}, Const<0>{}, 0);
+      step(Const<1>{}, s, Const<2>{}, Const<0>{}, 0);
+      step(Const<0>{}, s, Const<3>{}, Const<0>{}, 0);
+      prepare(kt + 2);
+      // vmcnt(0) lgkmcnt(0): the next K-tile has landed for this wave, and its
+      // reads of this one are done; after the barrier so for everyone
+      __builtin_amdgcn_s_waitcnt(0x0070);
+      block_barrier();
+      step(Const<1>{}, smem + (stage ^ STAGE), Const<0>{}, Const<1>{}, stage);
+      stage ^= STAGE;
+    }
   }
+  wait_vmcnt<0>();  // what the last steps loaded (nothing is read, zeros are written)
   __syncthreads();  // everyone is done with the operand tiles
 
   // Each block of 32 rows goes through the wave's own LDS region, so that a
@@ -412,13 +475,14 @@ __global__ __launch_bounds__(WM* WN * 64) void product_kernel(GemmArgs g) {
       load8<float>(q + r * PIT + c8, v);
       if constexpr (EPI == EPI_OUT) {
         if (row < g.M && col < g.N) {
-          if (g.splits > 1)
+          if (g.raw)
             store8<float>(g.partial + ((size_t)split * g.M + row) * g.ldp + col, v);
           else
             epi_out<T>(g.e, g.N, g.vec, row, col, v);
         }
       } else if constexpr (EPI == EPI_LSE) {
-        static_assert(EPI != EPI_LSE || FN * 32 == STAT_COLS, "a wave's columns are one group");
+        static_assert(FN * 32 % STAT_COLS == 0, "whole groups of columns");
+        constexpr int LPG = STAT_COLS / 8;  // lanes per group
         float m = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -426,15 +490,15 @@ __global__ __launch_bounds__(WM* WN * 64) void product_kernel(GemmArgs g) {
           m = fmaxf(m, v[j]);
         }
 #pragma unroll
-        for (int d = 1; d < LPR; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+        for (int d = 1; d < LPG; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
         const float ms = m == -INFINITY ? 0.f : m;
         float s = 0.f;  // NaN where a value is (fmaxf passed over it)
 #pragma unroll
         for (int j = 0; j < 8; ++j) s += exp_fast(v[j] - ms);
 #pragma unroll
-        for (int d = 1; d < LPR; d <<= 1) s += __shfl_xor(s, d);
+        for (int d = 1; d < LPG; d <<= 1) s += __shfl_xor(s, d);
         if (row < g.M) {
-          if (c8 == 0 && col < g.N) g.e.stats[(size_t)row * g.e.nstat + g.e.stat0 + col / STAT_COLS] = make_float2(m, s);
+          if (c8 % STAT_COLS == 0 && col < g.N) g.e.stats[(size_t)row * g.e.nstat + g.e.stat0 + col / STAT_COLS] = make_float2(m, s);
           const int lab = g.e.labels[row];
           const uint32_t at = (uint32_t)lab - (uint32_t)(g.e.col0 + col);
           if (at < 8u && label_ok(lab, g.e.classes)) {
@@ -534,7 +598,7 @@ template <typename T, bool AKC, bool BKC, int EPI> hipError_t launch_tiles(const
   const dim3 grid((unsigned)((long)g.tiles_m * g.tiles_n * g.splits));
   TraceScope ts(p.name, st, p.flops, WORK_FLOP);
   if (sizeof(T) == 2 && big)
-    hipLaunchKernelGGL((product_kernel<T, AKC, BKC, 2, 4, sizeof(T) == 2 ? 4 : 2, 2, EPI>), grid, dim3(512), 0, st, g);
+    hipLaunchKernelGGL((product_kernel<T, AKC, BKC, 2, 2, sizeof(T) == 2 ? 4 : 2, sizeof(T) == 2 ? 4 : 2, EPI>), grid, dim3(256), 0, st, g);
   else
     hipLaunchKernelGGL((product_kernel<T, AKC, BKC, 2, 2, 2, 2, EPI>), grid, dim3(256), 0, st, g);
   return hipGetLastError();
@@ -563,6 +627,7 @@ template <typename T> hipError_t launch_product_t(const Product& p, float* parti
   g.tiles_n = (p.N + bm - 1) / bm;
   g.partial = partial;
   g.ldp = ((long)p.N + 7) / 8 * 8;
+  g.raw = p.raw || g.splits > 1;
   g.vec = p.N % 8 == 0;
   g.e = p.e;
   if (!g.e.ldy) g.e.ldy = p.N;
@@ -575,7 +640,7 @@ template <typename T> hipError_t launch_product_t(const Product& p, float* parti
     e = p.epi == EPI_LSE ? launch_tiles<T, true, true, EPI_LSE>(p, g, pl.big, st)
                          : launch_tiles<T, true, true, EPI_DLOGITS>(p, g, pl.big, st);
   }
-  if (e != hipSuccess || g.splits == 1) return e;
+  if (e != hipSuccess || g.splits == 1 || p.raw) return e;
   TraceScope ts("product_reduce_kernel", st, 4.0 * (g.splits + 1) * p.M * p.N, WORK_BYTE);
   hipLaunchKernelGGL(product_reduce_kernel<T>, dim3((unsigned)(((long)p.M * (g.ldp / 8) + 255) / 256)), dim3(256), 0, st, g);
   return hipGetLastError();

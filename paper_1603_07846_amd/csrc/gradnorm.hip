@@ -6,7 +6,8 @@
 // call holds its own copy and nothing is copied to the device.  Each
 // workgroup sums the squares of one piece of one tensor in fp64 (the card's
 // fp64 rate is far above what the loads deliver, and no square overflows or
-// vanishes) into its own slot; one workgroup adds the slots in order.
+// vanishes) into its own slot; one workgroup adds the slots in order, or, when
+// clipping has few of them, every workgroup that scales does.
 #include "conv_common.h"
 #include "gradnorm.h"
 
@@ -110,17 +111,26 @@ __global__ __launch_bounds__(256) void grad_sq_kernel(List l, double* __restrict
   if (threadIdx.x == 0) slots[l.slot0 + blockIdx.x] = all;
 }
 
-__global__ __launch_bounds__(1024) void grad_norm_kernel(const double* __restrict__ slots, uint32_t n, float max_norm,
-                                                         float* __restrict__ stat) {
-  __shared__ double lds[16];
+// The norm and the scale from the slots, the same in every thread and for
+// every number of threads a multiple of 256 (thread t adds slots t, t + 256, ...
+// of the first 256 threads).
+__device__ __forceinline__ float2 norm_of(const double* __restrict__ slots, uint32_t n, float max_norm, double* lds) {
   double s = 0;
-  for (uint32_t i = threadIdx.x; i < n; i += 1024) s += slots[i];
-  s = wg_sum(s, lds, 16);
-  if (threadIdx.x) return;
-  const double norm = sqrt(s);
-  stat[0] = (float)norm;
+  if (threadIdx.x < 256)
+    for (uint32_t i = threadIdx.x; i < n; i += 256) s += slots[i];
+  const double norm = sqrt(wg_sum(s, lds, (int)blockDim.x / 64));
   // a norm that is not finite compares false, or is excluded
-  stat[1] = norm > (double)max_norm && norm <= 1.7976931348623157e308 ? (float)((double)max_norm / norm) : 1.f;
+  const bool over = norm > (double)max_norm && norm <= 1.7976931348623157e308;
+  return make_float2((float)norm, over ? (float)((double)max_norm / norm) : 1.f);
+}
+
+__global__ __launch_bounds__(256) void grad_norm_kernel(const double* __restrict__ slots, uint32_t n, float max_norm,
+                                                        float* __restrict__ stat) {
+  __shared__ double lds[4];
+  const float2 r = norm_of(slots, n, max_norm, lds);
+  if (threadIdx.x) return;
+  stat[0] = r.x;
+  stat[1] = r.y;
 }
 
 template <typename T> __device__ __forceinline__ void piece_scale(const T* p, T* o, uint64_t n, float s) {
@@ -154,10 +164,24 @@ template <typename T> __device__ __forceinline__ void piece_scale(const T* p, T*
   for (uint64_t j = head + nv * VEC + t; j < n; j += 256) store_out<T>(o + j, elem_f(p[j]) * s);
 }
 
-__global__ __launch_bounds__(256) void grad_scale_kernel(List l, const float* __restrict__ stat) {
+// n: number of slots to add here (0: stat is written already).  The first
+// workgroup of the first launch writes stat then.
+__global__ __launch_bounds__(256) void grad_scale_kernel(List l, float* __restrict__ stat, const double* __restrict__ slots,
+                                                         uint32_t n, float max_norm) {
+  __shared__ double lds[4];
   uint64_t lo, hi;
   const int i = find(l, blockIdx.x, lo, hi);
-  const float s = stat[1];
+  float s;
+  if (n) {
+    const float2 r = norm_of(slots, n, max_norm, lds);
+    s = r.y;
+    if (l.slot0 + blockIdx.x + threadIdx.x == 0) {
+      stat[0] = r.x;
+      stat[1] = r.y;
+    }
+  } else {
+    s = stat[1];
+  }
   const void* p = l.t[i].p;
   void* o = l.t[i].out;
   if (s == 1.f && p == o) return;
@@ -178,6 +202,7 @@ hipError_t launch_grad_norm(int count, const int* dt, const void* const* grads, 
   uint64_t piece = (total + NORM_PIECES - 1) / NORM_PIECES;
   piece = piece < 16384 ? 16384 : (piece + 8191) / 8192 * 8192;
   uint32_t slots_used = 0;
+  bool sum_here = false;
   for (int pass = 0; pass < (outs ? 2 : 1); ++pass) {
     uint32_t slot = 0;
     for (int at = 0; at < count;) {
@@ -197,7 +222,7 @@ hipError_t launch_grad_norm(int count, const int* dt, const void* const* grads, 
         hipLaunchKernelGGL(grad_sq_kernel, dim3(wgs), dim3(256), 0, st, l, slots);
       } else {
         TraceScope ts("grad_scale_kernel", st, 2 * bytes, WORK_BYTE);
-        hipLaunchKernelGGL(grad_scale_kernel, dim3(wgs), dim3(256), 0, st, l, stat);
+        hipLaunchKernelGGL(grad_scale_kernel, dim3(wgs), dim3(256), 0, st, l, stat, slots, sum_here ? slots_used : 0, max_norm);
       }
       bytes = 0;  // the trace counts the whole list at its first launch
       const hipError_t e = hipGetLastError();
@@ -205,11 +230,15 @@ hipError_t launch_grad_norm(int count, const int* dt, const void* const* grads, 
     }
     if (pass) break;
     slots_used = slot;
+    // A launch costs about 3 us; 512 slots are 4 KB that each workgroup reads
+    // from a cache in well under 1.
+    sum_here = outs && slots_used && slots_used <= 512;
+    for (int i = 0; i < count; ++i) bytes += (double)sizes[i] * dt_size(dt[i]);
+    if (sum_here) continue;
     TraceScope ts("grad_norm_kernel", st, 8.0 * slots_used, WORK_BYTE);
-    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(1024), 0, st, slots, slots_used, max_norm, stat);
+    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, st, slots, slots_used, max_norm, stat);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    for (int i = 0; i < count; ++i) bytes += (double)sizes[i] * dt_size(dt[i]);
   }
   return hipSuccess;
 }

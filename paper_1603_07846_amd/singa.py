@@ -12,6 +12,7 @@ fp32 tensors are torch.float32, bf16 tensors torch.bfloat16.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import functools
 import os
@@ -545,31 +546,53 @@ def adagrad_update(w, g, h, w_bf16=None, lr=0.01, delta=1e-6, weight_decay=0.0, 
 
 
 # ------------------------------------------------------------ dense layers
-def _dense(name, t, dtype, shape, current=None):
-    """t, if it is what the dense calls take: that dtype, that shape (None: any), contiguous, on the current device."""
-    if t.dtype != dtype:
+#
+# Calls of a few microseconds wait for their host side, so the checks are one
+# expression per tensor and say what is wrong only where something is.
+def _current() -> int:
+    return _raw_device() if _raw_device is not None else torch.cuda.current_device()
+
+
+def _current_stream(cur):
+    return _raw_stream(cur) if _raw_stream is not None and torch.cuda.is_initialized() else _stream()
+
+
+def _dense(name, t, dtype, shape, cur):
+    """t, if it is what the dense calls take: that dtype, that shape (None: any), contiguous, on the current GPU."""
+    if t.dtype is dtype and (shape is None or t.shape == shape) and t.is_contiguous() and t.get_device() == cur:
+        return t
+    if t.dtype is not dtype:
         raise TypeError("%s: %s wanted, got %s" % (name, dtype, t.dtype))
-    if shape is not None and tuple(t.shape) != shape:
-        raise ValueError("%s: shape %s wanted, got %s" % (name, shape, tuple(t.shape)))
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s: shape %s wanted, got %s" % (name, tuple(shape), tuple(t.shape)))
     if not t.is_contiguous():
         raise ValueError("%s: not contiguous" % name)
-    if not t.is_cuda or t.device.index != (_raw_device() if _raw_device is not None else torch.cuda.current_device()):
-        raise ValueError("%s: not on the current GPU (%s)" % (name, t.device))
-    return t
+    raise ValueError("%s: not on the current GPU (%s)" % (name, t.device))
 
 
 def _factor(t):
-    return _dense("grad_scale", t, torch.float32, (1,))
+    return _dense("grad_scale", t, torch.float32, (1,), _current())
+
+
+_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _dtype_code(dtype) -> int:
+    if dtype not in _CODES:
+        raise TypeError("unsupported dtype %s" % dtype)
+    return _CODES[dtype]
 
 
 def _rows(x, w):
-    """(dtype code, rows, in, out) of x (..., in) and w (out, in)."""
-    dt = _dt(x)
-    if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1] or w.shape[0] < 1 or w.shape[1] < 1:
-        raise ValueError("x (..., in) and w (out, in) wanted, got %s and %s" % (tuple(x.shape), tuple(w.shape)))
-    _dense("x", x, x.dtype, None)
-    _dense("w", w, x.dtype, None)
-    return dt, x.numel() // w.shape[1], w.shape[1], w.shape[0]
+    """(dtype code, current GPU, in, out) of x (..., in) and w (out, in)."""
+    dt = _dtype_code(x.dtype)
+    ws, xs = w.shape, x.shape
+    if len(ws) != 2 or not xs or xs[-1] != ws[1] or ws[0] < 1 or ws[1] < 1:
+        raise ValueError("x (..., in) and w (out, in) wanted, got %s and %s" % (tuple(xs), tuple(ws)))
+    cur = _current() if x.is_cuda else -2
+    _dense("x", x, x.dtype, None, cur)
+    _dense("w", w, x.dtype, None, cur)
+    return dt, cur, ws[1], ws[0]
 
 
 def _act(act) -> int:
@@ -579,21 +602,28 @@ def _act(act) -> int:
 
 
 def _dw_dt(x, dw_dtype) -> int:
-    if dw_dtype == torch.float32:
+    if dw_dtype is torch.float32:
         return F32
-    if dw_dtype == torch.bfloat16 and x.dtype == torch.bfloat16:
+    if dw_dtype is torch.bfloat16 and x.dtype is torch.bfloat16:
         return BF16
     raise TypeError("dw_dtype: torch.float32, or torch.bfloat16 with bf16 tensors, wanted, got %s" % dw_dtype)
 
 
-def _out(name, t, shape, dtype, device):
-    return empty(shape, dtype, device) if t is None else _dense(name, t, dtype, tuple(shape))
+def _out(name, t, shape, dtype, device, cur):
+    return _ALLOC(shape, dtype, device) if t is None else _dense(name, t, dtype, shape, cur)
 
 
-def _dense_ws(nbytes, device, ws):
-    if ws is not None and nbytes:
-        _dense("workspace", ws, torch.uint8, None)
-    return _workspace(nbytes, device, ws)
+def _dense_ws(nbytes, device, ws, cur):
+    """(tensor or None, address, bytes) of a workspace."""
+    if not nbytes:
+        return None, None, 0
+    if ws is None:
+        ws = _ALLOC((nbytes,), torch.uint8, device)
+    elif ws.dim() != 1:
+        raise ValueError("workspace: one dimension wanted")
+    else:
+        _dense("workspace", ws, torch.uint8, None, cur)
+    return ws, ws.data_ptr(), ws.numel()
 
 
 def _bytes(fn, *args) -> int:
@@ -604,48 +634,39 @@ def _bytes(fn, *args) -> int:
 
 @functools.lru_cache(maxsize=1024)
 def linear_fwd_workspace_bytes(dtype, rows, din, dout) -> int:
-    return _bytes("singa_linear_fwd_workspace_bytes", dtype if isinstance(dtype, int) else _dtype_code(dtype), rows, din,
-                  dout)
+    return _bytes("singa_linear_fwd_workspace_bytes", _dtype_code(dtype), rows, din, dout)
 
 
 @functools.lru_cache(maxsize=1024)
 def linear_bwd_workspace_bytes(dtype, rows, din, dout, act="none", dw_dtype=torch.float32) -> int:
-    return _bytes("singa_linear_bwd_workspace_bytes", dtype if isinstance(dtype, int) else _dtype_code(dtype), rows, din,
-                  dout, _act(act), _dtype_code(dw_dtype))
+    return _bytes("singa_linear_bwd_workspace_bytes", _dtype_code(dtype), rows, din, dout, _act(act), _dtype_code(dw_dtype))
 
 
 @functools.lru_cache(maxsize=1024)
 def linear_softmax_ce_workspace_bytes(dtype, rows, din, classes, grad=True, dw_dtype=torch.float32) -> int:
-    return _bytes("singa_linear_softmax_ce_workspace_bytes", dtype if isinstance(dtype, int) else _dtype_code(dtype), rows,
-                  din, classes, int(bool(grad)), _dtype_code(dw_dtype))
-
-
-def _dtype_code(dtype) -> int:
-    if dtype == torch.float32:
-        return F32
-    if dtype == torch.bfloat16:
-        return BF16
-    raise TypeError("unsupported dtype %s" % dtype)
+    return _bytes("singa_linear_softmax_ce_workspace_bytes", _dtype_code(dtype), rows, din, classes, int(bool(grad)),
+                  _dtype_code(dw_dtype))
 
 
 def linear_fwd(x, w, bias=None, act="none", residual=None, keep_z=False, out=None, z=None, workspace=None):
     """Inner product ComputeFeature: y = act(x w^T + bias) + residual, x (..., in), w (out, in), bias fp32.
     keep_z (or z, a tensor for it): also the pre-activation x w^T + bias, which linear_bwd takes; then (y, z) is
     returned.  act: "none", "relu", "gelu" (erf) or "silu"."""
-    dt, rows, din, dout = _rows(x, w)
-    a = _act(act)
-    shape = tuple(x.shape[:-1]) + (dout,)
+    dt, cur, din, dout = _rows(x, w)
+    a, dtype, device = _act(act), x.dtype, x.device
+    shape, rows = x.shape[:-1] + (dout,), x.numel() // din
     if bias is not None:
-        _dense("bias", bias, torch.float32, (dout,))
+        _dense("bias", bias, torch.float32, (dout,), cur)
     if residual is not None:
-        _dense("residual", residual, x.dtype, shape)
-    y = _out("out", out, shape, x.dtype, x.device)
+        _dense("residual", residual, dtype, shape, cur)
+    y = _out("out", out, shape, dtype, device, cur)
     if keep_z or z is not None:
-        z = _out("z", z, shape, x.dtype, x.device)
-    ws = _dense_ws(linear_fwd_workspace_bytes(dt, rows, din, dout), x.device, workspace)
-    _check("singa_linear_fwd", _lib().singa_linear_fwd(
-        dt, rows, din, dout, _ptr(x), _ptr(w), _ptr(bias), a, _ptr(residual), _ptr(z), _ptr(y), _ptr(ws),
-        0 if ws is None else ws.numel(), _stream()))
+        z = _out("z", z, shape, dtype, device, cur)
+    ws, at, nbytes = _dense_ws(linear_fwd_workspace_bytes(dtype, rows, din, dout), device, workspace, cur)
+    rc = _LIB.singa_linear_fwd(dt, rows, din, dout, x.data_ptr(), w.data_ptr(), _ptr(bias), a, _ptr(residual), _ptr(z),
+                               y.data_ptr(), at, nbytes, _current_stream(cur))
+    if rc:
+        raise SingaError("singa_linear_fwd", rc)
     return y if z is None else (y, z)
 
 
@@ -654,27 +675,29 @@ def linear_bwd(x, w, dy, act="none", z=None, dx_residual=None, need_dx=True, nee
     """Inner product ComputeGradient: (dx, dw, db) (None where not asked for) from dy, the gradient at the output,
     and the z that linear_fwd kept (not with act "none").  dx_residual: a gradient that reaches x another way,
     added to dx.  dw is fp32, or bf16 with dw_dtype; accumulate adds into the given dw (fp32) and db."""
-    dt, rows, din, dout = _rows(x, w)
-    a, gt = _act(act), _dw_dt(x, dw_dtype)
-    shape = tuple(x.shape[:-1]) + (dout,)
-    _dense("dy", dy, x.dtype, shape)
-    if act == "none":
+    dt, cur, din, dout = _rows(x, w)
+    a, gt, dtype, device = _act(act), _dw_dt(x, dw_dtype), x.dtype, x.device
+    shape, rows = x.shape[:-1] + (dout,), x.numel() // din
+    _dense("dy", dy, dtype, shape, cur)
+    if not a:
         z = None
     elif z is None:
         raise ValueError("z: the kept pre-activation is wanted with act %r" % act)
     else:
-        _dense("z", z, x.dtype, shape)
+        _dense("z", z, dtype, shape, cur)
     if dx_residual is not None:
-        _dense("dx_residual", dx_residual, x.dtype, tuple(x.shape))
+        _dense("dx_residual", dx_residual, dtype, x.shape, cur)
     if accumulate and ((need_dw and dw is None) or (with_bias and db is None)):
         raise ValueError("accumulate: the dw and db to add into are wanted")
-    dx = _out("dx", dx, tuple(x.shape), x.dtype, x.device) if need_dx else None
-    dw = _out("dw", dw, (dout, din), dw_dtype, x.device) if need_dw else None
-    db = _out("db", db, (dout,), torch.float32, x.device) if with_bias else None
-    ws = _dense_ws(linear_bwd_workspace_bytes(dt, rows, din, dout, act, dw_dtype), x.device, workspace)
-    _check("singa_linear_bwd", _lib().singa_linear_bwd(
-        dt, rows, din, dout, _ptr(x), _ptr(w), _ptr(z), a, _ptr(dy), _ptr(dx_residual), _ptr(dx), _ptr(dw), gt,
-        _ptr(db), int(bool(accumulate)), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+    dx = _out("dx", dx, x.shape, dtype, device, cur) if need_dx else None
+    dw = _out("dw", dw, (dout, din), dw_dtype, device, cur) if need_dw else None
+    db = _out("db", db, (dout,), torch.float32, device, cur) if with_bias else None
+    ws, at, nbytes = _dense_ws(linear_bwd_workspace_bytes(dtype, rows, din, dout, act, dw_dtype), device, workspace, cur)
+    rc = _LIB.singa_linear_bwd(dt, rows, din, dout, x.data_ptr(), w.data_ptr(), _ptr(z), a, dy.data_ptr(),
+                               _ptr(dx_residual), _ptr(dx), _ptr(dw), gt, _ptr(db), 1 if accumulate else 0, at, nbytes,
+                               _current_stream(cur))
+    if rc:
+        raise SingaError("singa_linear_bwd", rc)
     return dx, dw, db
 
 
@@ -684,58 +707,66 @@ def linear_softmax_ce(x, w, labels, bias=None, grad=True, need_dx=True, need_dw=
     dw, db) with loss as in softmax_ce (the mean over the counted rows, then each row's) and, with grad, the
     gradients of scale * loss (db when there is a bias).  A row whose label (int32, one per row) is outside
     [0, classes) is padding: not counted, loss and gradient zero.  dw_dtype, accumulate: as in linear_bwd."""
-    dt, rows, din, classes = _rows(x, w)
-    gt = _dw_dt(x, dw_dtype)
-    _dense("labels", labels, torch.int32, tuple(x.shape[:-1]))
+    dt, cur, din, classes = _rows(x, w)
+    gt, device, rows = _dw_dt(x, dw_dtype), x.device, x.numel() // din
+    _dense("labels", labels, torch.int32, x.shape[:-1], cur)
     if bias is not None:
-        _dense("bias", bias, torch.float32, (classes,))
+        _dense("bias", bias, torch.float32, (classes,), cur)
     need_dx, need_dw, need_db = grad and need_dx, grad and need_dw, grad and bias is not None
     if accumulate and ((need_dw and dw is None) or (need_db and db is None)):
         raise ValueError("accumulate: the dw and db to add into are wanted")
-    loss = _out("loss", loss, (rows + 1,), torch.float32, x.device)
-    dx = _out("dx", dx, tuple(x.shape), x.dtype, x.device) if need_dx else None
-    dw = _out("dw", dw, (classes, din), dw_dtype, x.device) if need_dw else None
-    db = _out("db", db, (classes,), torch.float32, x.device) if need_db else None
+    loss = _out("loss", loss, (rows + 1,), torch.float32, device, cur)
+    dx = _out("dx", dx, x.shape, x.dtype, device, cur) if need_dx else None
+    dw = _out("dw", dw, (classes, din), dw_dtype, device, cur) if need_dw else None
+    db = _out("db", db, (classes,), torch.float32, device, cur) if need_db else None
     any_grad = bool(need_dx or need_dw or need_db)
-    ws = _dense_ws(linear_softmax_ce_workspace_bytes(dt, rows, din, classes, any_grad, dw_dtype), x.device, workspace)
-    _check("singa_linear_softmax_ce", _lib().singa_linear_softmax_ce(
-        dt, rows, din, classes, _ptr(x), _ptr(w), _ptr(bias), _ptr(labels), float(scale), _ptr(loss), _ptr(dx), _ptr(dw),
-        gt, _ptr(db), int(bool(accumulate)), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+    ws, at, nbytes = _dense_ws(linear_softmax_ce_workspace_bytes(x.dtype, rows, din, classes, any_grad, dw_dtype), device,
+                               workspace, cur)
+    rc = _LIB.singa_linear_softmax_ce(dt, rows, din, classes, x.data_ptr(), w.data_ptr(), _ptr(bias), labels.data_ptr(),
+                                      scale, loss.data_ptr(), _ptr(dx), _ptr(dw), gt, _ptr(db), 1 if accumulate else 0, at,
+                                      nbytes, _current_stream(cur))
+    if rc:
+        raise SingaError("singa_linear_softmax_ce", rc)
     return loss, dx, dw, db
 
 
-def _grad_list(tensors, name):
-    for t in tensors:
-        if not t.is_contiguous() or not t.is_cuda:
-            raise ValueError("%s: contiguous tensors on the current GPU wanted" % name)
-    if tensors:
-        _dense(name, tensors[0], tensors[0].dtype, None)
-        if any(t.device != tensors[0].device for t in tensors):
-            raise ValueError("%s: tensors on one GPU wanted" % name)
-    n = len(tensors)
-    return (ctypes.c_void_p * n)(*[t.data_ptr() for t in tensors])
+def _grad_list(name, tensors, cur):
+    """(types, sizes, addresses) of the tensors, as lists."""
+    if False in [t.is_contiguous() for t in tensors] or [t.get_device() for t in tensors].count(cur) != len(tensors):
+        raise ValueError("%s: contiguous tensors on the current GPU wanted" % name)
+    try:
+        types = [_CODES[t.dtype] for t in tensors]
+    except KeyError as e:
+        raise TypeError("%s: unsupported dtype %s" % (name, e.args[0]))
+    return types, [t.numel() for t in tensors], [t.data_ptr() for t in tensors]
+
+
+def _c_array(kind, code, values):
+    return (kind * len(values)).from_buffer(array.array(code, values))
 
 
 def _grad_stat(grads, max_norm, out, stat, workspace):
-    grads = list(grads)
-    n = len(grads)
-    if not n:
+    if not grads:
         raise ValueError("grads: at least one tensor wanted")
-    ptrs = _grad_list(grads, "grads")
-    dtypes = (ctypes.c_int * n)(*[_dtype_code(t.dtype) for t in grads])
-    sizes = (ctypes.c_size_t * n)(*[t.numel() for t in grads])
-    device = grads[0].device
-    stat = _out("stat", stat, (2,), torch.float32, device)
-    ws = _dense_ws(_lib().singa_grad_norm_workspace_bytes(n), device, workspace)
+    n, device = len(grads), grads[0].device
+    cur = _current() if grads[0].is_cuda else -2
+    types, sizes, ptrs = _grad_list("grads", grads, cur)
+    outs = ptrs
+    if out is not None and out is not grads:
+        otypes, osizes, outs = _grad_list("out", out, cur)
+        if otypes != types or osizes != sizes:
+            raise ValueError("out: tensors of the gradients' sizes and types wanted")
+    stat = _out("stat", stat, (2,), torch.float32, device, cur)
+    ws, at, nbytes = _dense_ws(_LIB.singa_grad_norm_workspace_bytes(n), device, workspace, cur)
+    types, sizes = _c_array(ctypes.c_int, "i", types), _c_array(ctypes.c_size_t, "Q", sizes)
+    ptrs = _c_array(ctypes.c_void_p, "Q", ptrs)
     if out is None:
-        _check("singa_grad_norm", _lib().singa_grad_norm(n, dtypes, ptrs, sizes, float(max_norm), _ptr(stat), _ptr(ws),
-                                                         ws.numel(), _stream()))
-        return stat
-    out = list(out)
-    if len(out) != n or any(o.shape != g.shape or o.dtype != g.dtype for o, g in zip(out, grads)):
-        raise ValueError("out: tensors of the gradients' shapes and types wanted")
-    _check("singa_grad_clip", _lib().singa_grad_clip(n, dtypes, ptrs, _grad_list(out, "out"), sizes, float(max_norm),
-                                                     _ptr(stat), _ptr(ws), ws.numel(), _stream()))
+        rc = _LIB.singa_grad_norm(n, types, ptrs, sizes, max_norm, stat.data_ptr(), at, nbytes, _current_stream(cur))
+    else:
+        rc = _LIB.singa_grad_clip(n, types, ptrs, _c_array(ctypes.c_void_p, "Q", outs), sizes, max_norm, stat.data_ptr(),
+                                  at, nbytes, _current_stream(cur))
+    if rc:
+        raise SingaError("singa_grad_norm" if out is None else "singa_grad_clip", rc)
     return stat
 
 
@@ -743,13 +774,13 @@ def grad_norm(grads, max_norm=float("inf"), stat=None, workspace=None):
     """The global norm over all gradient tensors (fp32 and bf16, mixed) and the factor that clips it to max_norm: an
     fp32 device tensor (norm, scale), scale = max_norm / norm where norm > max_norm and is finite, else 1.  The
     updates take stat[1:] as grad_scale."""
-    return _grad_stat(grads, max_norm, None, stat, workspace)
+    return _grad_stat(list(grads), max_norm, None, stat, workspace)
 
 
 def clip_grads(grads, max_norm, out=None, stat=None, workspace=None):
     """grad_norm, then out[i] = scale * grads[i] (in place without out).  Returns (norm, scale) as grad_norm."""
     grads = list(grads)
-    return _grad_stat(grads, max_norm, grads if out is None else out, stat, workspace)
+    return _grad_stat(grads, max_norm, grads if out is None else list(out), stat, workspace)
 
 
 def trace_enable(on: bool = True):
