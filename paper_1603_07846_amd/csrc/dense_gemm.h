@@ -135,68 +135,132 @@ __device__ __forceinline__ void store_terms(T* y, bf16_t* more, size_t o, size_t
 
 __device__ __forceinline__ bool label_ok(int lab, int classes) { return lab >= 0 && lab < classes; }
 
-// EPI_OUT on 8 columns from col of one row; vec: N % 8 == 0 and every tensor
-// starts at a 16-byte boundary.
+// What EPI_OUT adds to or multiplies with a lane's 8 columns in every row.
+struct Columns {
+  float alpha, bias[8];
+};
+__device__ __forceinline__ Columns columns_of(const Epilogue& e, int N, int col) {
+  Columns c;
+  c.alpha = e.alpha ? e.alpha[0] : 1.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) c.bias[j] = e.bias && col + j < N ? e.bias[col + j] : 0.f;
+  return c;
+}
+
+// What EPI_OUT adds to 8 values of a row (the residual, or what y holds): two
+// 16-byte vectors of fp32, or one of bf16.
+struct Extra {
+  uint4 a, b;
+};
+template <typename T> __device__ __forceinline__ Extra load_extra(const Epilogue& e, int N, int row, int col, bool in) {
+  // every lane reads (element 0 stands in for what lies outside), so that no
+  // load sits in a branch that the next one waits for
+  Extra x;
+  if (e.add) {
+    const float* p = (const float*)e.y + (in ? (size_t)row * e.ldy + col : 0);
+    x.a = *(const uint4*)p;
+    x.b = *(const uint4*)(p + 4);
+  } else {
+    const T* p = (const T*)e.res + (in ? (size_t)row * N + col : 0);
+    x.a = *(const uint4*)p;
+    x.b = sizeof(T) == 4 ? *(const uint4*)(p + 4) : x.a;
+  }
+  return x;
+}
+template <typename T> __device__ __forceinline__ void add_extra(bool f32, const Extra& x, float (&v)[8]) {
+  const uint32_t a[4] = {x.a.x, x.a.y, x.a.z, x.a.w}, b[4] = {x.b.x, x.b.y, x.b.z, x.b.w};
+  if (sizeof(T) == 4 || f32) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[j] += __uint_as_float(a[j]);
+      v[4 + j] += __uint_as_float(b[j]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[2 * j] += __uint_as_float(a[j] << 16);
+      v[2 * j + 1] += __uint_as_float(a[j] & 0xffff0000u);
+    }
+  }
+}
+
+// The activation of n values: one branch for all, so that their chains of
+// dependent instructions overlap.
+template <typename T, int n> __device__ __forceinline__ void act_all(float (&v)[n], int act) {
+  if (act == ACT_RELU) {
+#pragma unroll
+    for (int j = 0; j < n; ++j) v[j] = act_f<T>(v[j], ACT_RELU);
+  } else if (act == ACT_GELU) {
+#pragma unroll
+    for (int j = 0; j < n; ++j) v[j] = act_f<T>(v[j], ACT_GELU);
+  } else if (act == ACT_SILU) {
+#pragma unroll
+    for (int j = 0; j < n; ++j) v[j] = act_f<T>(v[j], ACT_SILU);
+  }
+}
+
+// EPI_OUT on 8 columns from col of R rows `step` apart, in 16-byte vectors
+// (N % 8 == 0 and every tensor starts at a 16-byte boundary).  x: what is
+// added (e.res or e.add); live: false where a label takes the row out.
+template <typename T, int R>
+__device__ __forceinline__ void epi_out(const Epilogue& e, int M, int N, int row0, int step, int col, float (&v)[R][8],
+                                        const Columns& c, const Extra (&x)[R], const bool (&live)[R]) {
+#pragma unroll
+  for (int u = 0; u < R; ++u)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[u][j] = fmaf(v[u][j], c.alpha, c.bias[j]);
+  if (e.z) {
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+      const int row = row0 + u * step;
+      if (row < M && col < N) store8<T>((T*)e.z + (size_t)row * N + col, v[u]);
+    }
+  }
+  if (e.act) {
+#pragma unroll
+    for (int u = 0; u < R; ++u) act_all<T, 8>(v[u], e.act);
+  }
+  if (e.labels) {
+#pragma unroll
+    for (int u = 0; u < R; ++u)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[u][j] = live[u] ? v[u][j] : 0.f;
+  }
+  if (e.res || e.add) {
+#pragma unroll
+    for (int u = 0; u < R; ++u) add_extra<T>(e.add, x[u], v[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < R; ++u) {
+    const int row = row0 + u * step;
+    const size_t o = (size_t)row * e.ldy + col;
+    if (row < M && col < N) {
+      if (e.out_f32)
+        store8<float>((float*)e.y + o, v[u]);
+      else
+        store8<T>((T*)e.y + o, v[u]);
+    }
+  }
+}
+
+// The same, element by element, for any N.
 template <typename T>
-__device__ __forceinline__ void epi_out(const Epilogue& e, int N, bool vec, int row, int col, float (&v)[8]) {
-  const size_t o = (size_t)row * N + col;
-  const size_t oy = (size_t)row * e.ldy + col;
-  const bool live = !e.labels || label_ok(e.labels[row], e.classes);
-  const int n = min(8, N - col);
-  if (e.alpha) {
-    const float alpha = e.alpha[0];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= alpha;
-  }
-  if (e.bias) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < n) v[j] += e.bias[col + j];
-  }
-  if (vec) {
-    if (e.z) store8<T>((T*)e.z + o, v);
-    if (e.act) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = act_f<T>(v[j], e.act);
-    }
-    if (e.res) {
-      float r[8];
-      load8<T>((const T*)e.res + o, r);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += r[j];
-    }
-    if (!live) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = 0.f;
-    }
-    if (e.out_f32) {
-      float* y = (float*)e.y + oy;
-      if (e.add) {
-        float r[8];
-        load8<float>(y, r);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += r[j];
-      }
-      store8<float>(y, v);
-    } else {
-      store8<T>((T*)e.y + oy, v);
-    }
-    return;
-  }
+__device__ __forceinline__ void epi_out_any(const Epilogue& e, int N, int row, int col, const float (&v)[8], const Columns& c,
+                                            bool live) {
+  const size_t o = (size_t)row * N + col, oy = (size_t)row * e.ldy + col;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    if (j >= n) break;
-    float x = v[j];
-    if (e.z) store_out<T>((T*)e.z + o + j, x);
-    if (e.act) x = act_f<T>(x, e.act);
-    if (e.res) x += elem_f(((const T*)e.res)[o + j]);
-    if (!live) x = 0.f;
-    if (e.out_f32) {
-      float* y = (float*)e.y + oy + j;
-      *y = e.add ? *y + x : x;
-    } else {
-      store_out<T>((T*)e.y + oy + j, x);
-    }
+    if (col + j >= N) break;
+    float y = fmaf(v[j], c.alpha, c.bias[j]);
+    if (e.z) store_out<T>((T*)e.z + o + j, y);
+    if (e.act) y = act_f<T>(y, e.act);
+    if (!live) y = 0.f;
+    if (e.res) y += elem_f(((const T*)e.res)[o + j]);
+    if (e.add) y += ((const float*)e.y)[oy + j];
+    if (e.out_f32)
+      ((float*)e.y)[oy + j] = y;
+    else
+      store_out<T>((T*)e.y + oy + j, y);
   }
 }
 
@@ -261,15 +325,6 @@ template <typename T, bool KC, int R, int NW> struct Tile {
         if (chunk(wave, lane, i) >= kleft) off[i] = OOB;
     }
   }
-  // the rsrc of K-tile kt: the tile's corner, and the bytes from there to the
-  // operand's end; none where the K-tile is not wanted
-  __device__ __forceinline__ static __amdgpu_buffer_rsrc_t rsrc(const char* p, long ld, long end, int r0, int kt, bool live) {
-    const long at = KC ? (long)r0 * ld + (long)kt * 128 : (long)kt * BK * ld + (long)r0 * ES;
-    const long left = end - at;
-    uint32_t n = left > 0x7ffffff0L ? 0x7ffffff0u : (uint32_t)left;
-    if (!live || left <= 0) n = 0;
-    return make_rsrc(p + at, n);
-  }
   // instruction i of this wave; lds: the LDS address of the wave's part
   __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, uint32_t lds, int i) const {
     asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + i * 1024), "v"(off[i]), "s"(rs)
@@ -322,16 +377,19 @@ template <typename T, bool KC, int R, int F> struct Frags {
 // Between the instructions of a step the wave reads the fragments of the next
 // one, so the matrix unit does not wait for LDS; the barrier of a K-tile comes
 // before its last step, whose instructions cover the first reads of the next
-// K-tile and the issue of the loads of the one after that, into the stage that
-// the barrier has freed.  Loads have a whole K-tile's time to land.
+// K-tile and the issue of the first loads of the one after that, into the stage
+// that the barrier has freed; the other loads follow in the next step (64 KB in
+// one step of 512 cycles were twice what the vector memory path takes: 870 ->
+// 833 us at 8192^3).  A barrier waits for loads issued at least two steps ago.
 template <typename T, bool AKC, bool BKC, int WM, int WN, int FM, int FN, int EPI>
-__global__ __launch_bounds__(WM* WN * 64) void product_kernel(GemmArgs g) {
+__global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(GemmArgs g) {
   constexpr int NW = WM * WN, BM = WM * FM * 32, BN = WN * FN * 32;
   typedef Tile<T, AKC, BM, NW> TA;
   typedef Tile<T, BKC, BN, NW> TB;
   constexpr int STAGE = TA::BYTES + TB::BYTES;
-  constexpr int PIT = FN * 32 + 8;  // floats per staged row: rows 4 apart lie half the banks apart
-  constexpr int SMEM = 2 * STAGE > NW * 32 * PIT * 4 ? 2 * STAGE : NW * 32 * PIT * 4;
+  constexpr int PIT = FN == 4 ? 152 : 88, HALF = FN * 16 + 16;  // floats per staged row; where its odd groups start
+  static_assert((FN == 2 || FN == 4) && PIT % 16 == 8 && PIT >= HALF + FN * 16, "rows 4 apart lie half the banks apart");
+  constexpr int SMEM = 2 * STAGE > NW * 32 * PIT * 4 + BM * 8 ? 2 * STAGE : NW * 32 * PIT * 4 + BM * 8;
   __shared__ __align__(1024) char smem[SMEM];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -367,21 +425,56 @@ __global__ __launch_bounds__(WM* WN * 64) void product_kernel(GemmArgs g) {
   const int kt0 = split * g.kt_split, kt1 = min(g.kt_all, kt0 + g.kt_split);
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem);
   const uint32_t lds_a = lds0 + wave * TA::NI * 1024, lds_b = lds0 + TA::BYTES + wave * TB::NI * 1024;
+  // Where the next K-tile to load starts in each operand, and the bytes from
+  // there to the operand's end (a load past it reads zeros); advanced K-tile by
+  // K-tile in scalar registers, in four parts that go between the matrix
+  // instructions.  Past the last K-tile nothing is left: no traffic.
+  const long step_a = AKC ? 128 : TA::BK * g.lda, step_b = BKC ? 128 : TB::BK * g.ldb;
+  const char *pa, *pb;
+  long left_a, left_b;
+  int kt_next = kt0, kb_next = kt0;
+  static_assert(TERMS == 3, "two places where B starts again");
+  if (g.wrap && kb_next >= g.wrap) kb_next -= g.wrap;
+  if (g.wrap && kb_next >= g.wrap) kb_next -= g.wrap;
+  {
+    const long at = (AKC ? (long)m0 * g.lda : (long)m0 * TA::ES) + kt0 * step_a;
+    const long bt = (BKC ? (long)n0 * g.ldb : (long)n0 * TB::ES) + kb_next * step_b;
+    pa = g.a + at;
+    pb = g.b + bt;
+    left_a = g.enda - at;
+    left_b = g.endb - bt;
+  }
   __amdgpu_buffer_rsrc_t ra, rb;
-  // what loading K-tile kt takes
-  auto prepare = [&](int kt) {
-    int kb = kt;  // the K-tile of B
-    static_assert(TERMS == 3, "two places where B starts again");
-    if (g.wrap && kb >= g.wrap) kb -= g.wrap;
-    if (g.wrap && kb >= g.wrap) kb -= g.wrap;
-    ra = TA::rsrc(g.a, g.lda, g.enda, m0, kt, kt < kt1);
-    rb = TB::rsrc(g.b, g.ldb, g.endb, n0, kb, kt < kt1);
+  auto clamp = [&](long left) {
+    const int n = left > 0x7ffffff0L ? 0x7ffffff0 : (int)left;
+    return (uint32_t)(kt_next < kt1 && left > 0 ? n : 0);
+  };
+  auto prepare = [&](int part) {
+    if (part == 0) ra = make_rsrc(pa, clamp(left_a));
+    if (part == 1) {
+      pa += step_a;
+      left_a -= step_a;
+    }
+    if (part == 2) rb = make_rsrc(pb, clamp(left_b));
+    if (part == 3) {
+      ++kb_next;
+      const bool again = kb_next == g.wrap;
+      const long d = again ? step_b - g.wrap * step_b : step_b;
+      kb_next = again ? 0 : kb_next;
+      pb += d;
+      left_b -= d;
+      ++kt_next;
+    }
+  };
+  // before the last K-tile is loaded: it may hold less of K
+  auto mask = [&](int kt) {
     if ((AKC || BKC) && kt == g.kt_all - 1) {
       ta.mask(wave, lane, g.kca - kt * 8);
-      tb.mask(wave, lane, g.kcb - kb * 8);
+      tb.mask(wave, lane, g.kcb - kt * 8);
     }
   };
   constexpr int NL = TA::NI + TB::NI;
+  constexpr int NLA = NL / 2;  // loaded in a K-tile's last step; the others in the next one's first
   auto load = [&](int i, uint32_t stage) {
     if (i < TA::NI)
       ta.load(ra, lds_a + stage, i);
@@ -390,10 +483,13 @@ __global__ __launch_bounds__(WM* WN * 64) void product_kernel(GemmArgs g) {
   };
   typename Chunk<T>::type af[2][FM], bf[2][FN];
   // the matrix instructions of one step on fragments `cur`, with the reads of
-  // step ks at s into the other set and, with LOADS, all loads in between
-  auto step = [&](auto cur_, const char* s, auto ks_, auto loads_, uint32_t stage) {
+  // step ks at s into the other set and, in between, what `with` says: 1: the
+  // next loads are prepared; 2, 3: their first and second half
+  auto step = [&](auto cur_, const char* s, auto ks_, auto with_, uint32_t stage) {
     constexpr int cur = decltype(cur_)::value, nxt = cur ^ 1, ks = decltype(ks_)::value, N = FM * FN;
-    constexpr bool LOADS = decltype(loads_)::value;
+    constexpr bool PREPARE = decltype(with_)::value == 1;
+    constexpr int L0 = decltype(with_)::value == 2 ? 0 : decltype(with_)::value == 3 ? NLA : 0;
+    constexpr int L1 = decltype(with_)::value == 2 ? NLA : decltype(with_)::value == 3 ? NL : 0;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       // fragments in the order in which the next step wants them
@@ -404,22 +500,26 @@ __global__ __launch_bounds__(WM* WN * 64) void product_kernel(GemmArgs g) {
         else
           af[nxt][f - FN] = fa.read(s, f - FN, ks);
       }
-      if constexpr (LOADS) {
-#pragma unroll
-        for (int l = n * NL / N; l < (n + 1) * NL / N; ++l) load(l, stage);
+      if constexpr (PREPARE) {
+        if (n % (N / 4) == 0) prepare(n / (N / 4));
       }
+#pragma unroll
+      for (int l = L0 + n * (L1 - L0) / N; l < L0 + (n + 1) * (L1 - L0) / N; ++l) load(l, stage);
       mma32(af[cur][n / FN], bf[cur][n % FN], acc[n / FN][n % FN]);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
   if (kt0 < kt1) {
-    prepare(kt0);
+    // the first K-tile, and of the second what a last step loads
+    mask(kt0);
+    for (int part = 0; part < 4; ++part) prepare(part);
 #pragma unroll
     for (int i = 0; i < NL; ++i) load(i, 0);
-    prepare(kt0 + 1);
+    mask(kt0 + 1);
+    for (int part = 0; part < 4; ++part) prepare(part);
 #pragma unroll
-    for (int i = 0; i < NL; ++i) load(i, STAGE);
-    wait_vmcnt<NL>();  // the first K-tile has landed for this wave
+    for (int i = 0; i < NLA; ++i) load(i, STAGE);
+    wait_vmcnt<NLA>();  // the first K-tile has landed for this wave
     block_barrier();   // ... and for everyone
 #pragma unroll
     for (int b = 0; b < FN; ++b) bf[0][b] = fb.read(smem + TA::BYTES, b, 0);
@@ -428,15 +528,15 @@ __global__ __launch_bounds__(WM* WN * 64) void product_kernel(GemmArgs g) {
     uint32_t stage = 0;
     for (int kt = kt0; kt < kt1; ++kt) {
       const char* s = smem + stage;
-      step(Const<0>{}, s, Const<1>{}, Const<0>{}, 0);
-      step(Const<1>{}, s, Const<2>{}, Const<0>{}, 0);
+      step(Const<0>{}, s, Const<1>{}, Const<3>{}, stage ^ STAGE);
+      step(Const<1>{}, s, Const<2>{}, Const<1>{}, 0);
       step(Const<0>{}, s, Const<3>{}, Const<0>{}, 0);
-      prepare(kt + 2);
+      mask(kt + 2);
       // vmcnt(0) lgkmcnt(0): the next K-tile has landed for this wave, and its
       // reads of this one are done; after the barrier so for everyone
       __builtin_amdgcn_s_waitcnt(0x0070);
       block_barrier();
-      step(Const<1>{}, smem + (stage ^ STAGE), Const<0>{}, Const<1>{}, stage);
+      step(Const<1>{}, smem + (stage ^ STAGE), Const<0>{}, Const<2>{}, stage);
       stage ^= STAGE;
     }
   }
@@ -444,83 +544,176 @@ __global__ __launch_bounds__(WM* WN * 64) void product_kernel(GemmArgs g) {
   __syncthreads();  // everyone is done with the operand tiles
 
   // Each block of 32 rows goes through the wave's own LDS region, so that a
-  // lane holds 8 consecutive columns of a row.
+  // lane holds 8 consecutive columns of a row.  A staged row holds the even
+  // groups of 4 columns, then the odd ones: a lane's two 16-byte reads, and the
+  // rows' writes, meet every bank once.
   float* const q = (float*)(smem + wave * 32 * PIT * 4);
-  constexpr int LPR = FN * 4;        // lanes per row
-  constexpr int RPP = 64 / LPR;      // rows per pass
+  constexpr int LPR = FN * 4;    // lanes per row
+  constexpr int RPP = 64 / LPR;  // rows per pass
+  constexpr int UN = 32 / RPP;   // passes of a block
   const int li = lane & 31, lh = lane >> 5;
   const int c8 = (lane % LPR) * 8, rr = lane / LPR;
   const int col = n0 + wn * FN * 32 + c8;
-  float bv[8], cs[8];
-  if constexpr (EPI != EPI_OUT) {
+  const int wcol = (li & 3) + ((li >> 3) << 2) + (li & 4 ? HALF : 0);
+  auto read = [&](int r, float (&v)[8]) {
+    const float* s = q + r * PIT + c8 / 2;
+    const f32x4 a = *(const f32x4*)s, b = *(const f32x4*)(s + HALF);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = a[j], v[4 + j] = b[j];
+  };
+  Columns cols{};
+  float cs[8];
+  if constexpr (EPI == EPI_OUT) {
+    cols = columns_of(g.e, g.N, col);
+  } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      bv[j] = g.e.bias && col + j < g.N ? g.e.bias[col + j] : 0.f;
+      cols.bias[j] = g.e.bias && col + j < g.N ? g.e.bias[col + j] : 0.f;
       cs[j] = 0.f;
     }
   }
-#pragma unroll
-  for (int bm = 0; bm < FM; ++bm) {
-    const int row0 = m0 + (wm * FM + bm) * 32;
+  const bool edge = n0 + BN > g.N;  // columns past the end
+  // Stores count as outstanding like loads, and a wait for a load waits for
+  // every store before it: so what the rows take besides their sums is loaded
+  // before the first store (the rows' labels and lse go through LDS), and what
+  // is added to them a whole block at a time.
+  struct RowInfo {
+    int lab;
+    float lse;
+  };
+  RowInfo* const info = (RowInfo*)(smem + NW * 32 * PIT * 4);
+  const bool rows_have = EPI != EPI_OUT || g.e.labels;
+  if (rows_have) {
+    for (int r = threadIdx.x; r < BM; r += NW * 64) {
+      const int row = m0 + r;
+      RowInfo i{-1, 0.f};
+      if (row < g.M) {
+        i.lab = g.e.labels[row];
+        if constexpr (EPI == EPI_DLOGITS) i.lse = g.e.lse[row];
+      }
+      info[r] = i;
+    }
+  }
+  __syncthreads();
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0): the columns' values too
+  auto stage_block = [&](auto bm_) {
+    constexpr int bm = decltype(bm_)::value;
 #pragma unroll
     for (int bn = 0; bn < FN; ++bn)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) q[(8 * (v >> 2) + 4 * lh + (v & 3)) * PIT + bn * 32 + li] = acc[bm][bn][v];
+      for (int v = 0; v < 16; ++v) q[(8 * (v >> 2) + 4 * lh + (v & 3)) * PIT + bn * 16 + wcol] = acc[bm][bn][v];
+  };
+  // The accumulators' registers need constant indexes, the rest does not: one
+  // copy of it, which stays in the instruction cache.
+#pragma unroll 1
+  for (int bm = 0; bm < FM; ++bm) {
+    const int row0 = m0 + (wm * FM + bm) * 32;
+    Extra extra[UN];
+    if constexpr (EPI == EPI_OUT) {
+      if (g.vec && !g.raw && (g.e.res || g.e.add)) {
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+          const int row = row0 + u * RPP + rr;
+          extra[u] = load_extra<T>(g.e, g.N, row, col, row < g.M && col < g.N);
+        }
+      }
+    }
+    if (bm == 0) stage_block(Const<0>{});
+    if (bm == 1) stage_block(Const<1>{});
+    if constexpr (FM == 4) {
+      if (bm == 2) stage_block(Const<2>{});
+      if (bm == 3) stage_block(Const<3>{});
+    }
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's LDS writes are done
     __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-    for (int pass = 0; pass < 32 / RPP; ++pass) {
-      const int r = pass * RPP + rr, row = row0 + r;
-      float v[8];
-      load8<float>(q + r * PIT + c8, v);
-      if constexpr (EPI == EPI_OUT) {
-        if (row < g.M && col < g.N) {
-          if (g.raw)
-            store8<float>(g.partial + ((size_t)split * g.M + row) * g.ldp + col, v);
-          else
-            epi_out<T>(g.e, g.N, g.vec, row, col, v);
+    if constexpr (EPI == EPI_OUT) {
+      if (g.raw) {
+        float v[UN][8];
+#pragma unroll
+        for (int u = 0; u < UN; ++u) read(u * RPP + rr, v[u]);
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+          const int row = row0 + u * RPP + rr;
+          if (row < g.M && col < g.N) store8<float>(g.partial + ((size_t)split * g.M + row) * g.ldp + col, v[u]);
         }
-      } else if constexpr (EPI == EPI_LSE) {
-        static_assert(FN * 32 % STAT_COLS == 0, "whole groups of columns");
-        constexpr int LPG = STAT_COLS / 8;  // lanes per group
-        float m = -INFINITY;
+      } else if (g.vec) {
+        float v[UN][8];
+        bool live[UN];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          v[j] = col + j < g.N ? v[j] + bv[j] : -INFINITY;
-          m = fmaxf(m, v[j]);
+        for (int u = 0; u < UN; ++u) {
+          const int r = u * RPP + rr;
+          read(r, v[u]);
+          live[u] = !rows_have || label_ok(info[row0 + r - m0].lab, g.e.classes);
         }
-#pragma unroll
-        for (int d = 1; d < LPG; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-        const float ms = m == -INFINITY ? 0.f : m;
-        float s = 0.f;  // NaN where a value is (fmaxf passed over it)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s += exp_fast(v[j] - ms);
-#pragma unroll
-        for (int d = 1; d < LPG; d <<= 1) s += __shfl_xor(s, d);
-        if (row < g.M) {
-          if (c8 % STAT_COLS == 0 && col < g.N) g.e.stats[(size_t)row * g.e.nstat + g.e.stat0 + col / STAT_COLS] = make_float2(m, s);
-          const int lab = g.e.labels[row];
-          const uint32_t at = (uint32_t)lab - (uint32_t)(g.e.col0 + col);
-          if (at < 8u && label_ok(lab, g.e.classes)) {
-            float z = v[0];
-#pragma unroll
-            for (int j = 1; j < 8; ++j) z = at == (uint32_t)j ? v[j] : z;
-            g.e.zlab[row] = z;
-          }
-        }
+        epi_out<T, UN>(g.e, g.M, g.N, row0 + rr, RPP, col, v, cols, extra, live);
       } else {
-        const int lab = row < g.M ? g.e.labels[row] : -1;
-        const bool live = label_ok(lab, g.e.classes);
-        const float lse = live ? g.e.lse[row] : 0.f;
-        const uint32_t at = (uint32_t)lab - (uint32_t)(g.e.col0 + col);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float p = exp_fast(v[j] + bv[j] - lse) - (at == (uint32_t)j ? 1.f : 0.f);
-          v[j] = live && col + j < g.N ? p : 0.f;
-          cs[j] += v[j];
+#pragma unroll 1
+        for (int u = 0; u < UN; ++u) {
+          const int r = u * RPP + rr, row = row0 + r;
+          const bool live = !rows_have || label_ok(info[row - m0].lab, g.e.classes);
+          float v[8];
+          read(r, v);
+          if (row < g.M && col < g.N) epi_out_any<T>(g.e, g.N, row, col, v, cols, live);
         }
-        if (row < g.e.rows_padded && col < g.e.ldy) {
-          store_terms<T>((T*)g.e.y, g.e.more, (size_t)row * g.e.ldy + col, (size_t)g.e.rows_padded * g.e.ldy, v);
+      }
+    } else {
+      float vs[UN][8];
+      RowInfo ris[UN];
+#pragma unroll
+      for (int u = 0; u < UN; ++u) {
+        read(u * RPP + rr, vs[u]);
+        ris[u] = info[row0 + u * RPP + rr - m0];
+      }
+#pragma unroll
+      for (int u = 0; u < UN; ++u) {
+        const int row = row0 + u * RPP + rr;
+        const RowInfo ri = ris[u];
+        float(&v)[8] = vs[u];
+        const bool live = label_ok(ri.lab, g.e.classes);
+        const uint32_t at = (uint32_t)ri.lab - (uint32_t)(g.e.col0 + col);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += cols.bias[j];
+        if constexpr (EPI == EPI_LSE) {
+          static_assert(FN * 32 % STAT_COLS == 0, "whole groups of columns");
+          constexpr int LPG = STAT_COLS / 8;  // lanes per group
+          if (edge) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = col + j < g.N ? v[j] : -INFINITY;
+          }
+          float m = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+#pragma unroll
+          for (int d = 1; d < LPG; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+          const float ms = m == -INFINITY ? 0.f : m;
+          float s = 0.f;  // NaN where a value is (fmaxf passed over it)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) s += exp_fast(v[j] - ms);
+#pragma unroll
+          for (int d = 1; d < LPG; d <<= 1) s += __shfl_xor(s, d);
+          if (row < g.M) {
+            if (c8 % STAT_COLS == 0 && col < g.N)
+              g.e.stats[(size_t)row * g.e.nstat + g.e.stat0 + col / STAT_COLS] = make_float2(m, s);
+            if (at < 8u && live) {
+              float z = v[0];
+#pragma unroll
+              for (int j = 1; j < 8; ++j) z = at == (uint32_t)j ? v[j] : z;
+              g.e.zlab[row] = z;
+            }
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = exp_fast(v[j] - ri.lse);
+          if (at < 8u) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] -= at == (uint32_t)j ? 1.f : 0.f;
+          }
+          if (edge || !live) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = live && col + j < g.N ? v[j] : 0.f;
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) cs[j] += v[j];
+          if (row < g.e.rows_padded && col < g.e.ldy)
+            store_terms<T>((T*)g.e.y, g.e.more, (size_t)row * g.e.ldy + col, (size_t)g.e.rows_padded * g.e.ldy, v);
         }
       }
     }
@@ -562,7 +755,15 @@ template <typename T> __global__ __launch_bounds__(256) void product_reduce_kern
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] += u[j];
   }
-  epi_out<T>(g.e, g.N, g.vec, row, col, v);
+  const bool live = !g.e.labels || label_ok(g.e.labels[row], g.e.classes);
+  const Columns c = columns_of(g.e, g.N, col);
+  if (!g.vec) return epi_out_any<T>(g.e, g.N, row, col, v, c, live);
+  Extra x[1];
+  float v1[1][8];
+  if (g.e.res || g.e.add) x[0] = load_extra<T>(g.e, g.N, row, col, true);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v1[0][j] = v[j];
+  epi_out<T, 1>(g.e, g.M, g.N, row, 0, col, v1, c, x, {live});
 }
 
 struct Plan {
