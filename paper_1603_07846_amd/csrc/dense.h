@@ -105,6 +105,9 @@ hipError_t launch_zero(void* p, size_t bytes, hipStream_t st);
 // valid label (labels given) become zero.
 hipError_t launch_pack(int dt, const void* in, void* out, long rows, int cols, long ldo, const int32_t* labels,
                        int classes, hipStream_t st);
+// Two matrices of equal row length at once (no labels).
+hipError_t launch_pack2(int dt, const void* in, void* out, long rows, const void* in2, void* out2, long rows2, int cols,
+                        long ldo, hipStream_t st);
 // dz = dy act'(z) as T [rows_padded][ldz] (zero past rows and cols), more (may
 // be null) its further terms, colsum [ceil(rows / COLSUM_ROWS)][cols]
 // (may be null) the sums of the unrounded dz; dz may be null.

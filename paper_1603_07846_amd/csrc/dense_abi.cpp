@@ -230,8 +230,7 @@ int singa_linear_fwd(singa_dtype dtype, int rows, int in, int out, const void* x
   }
   hipError_t e = hipSuccess;
   if (o.k.copy) {
-    e = launch_pack(dtype, x, o.xp, rows, in, o.k.ld, nullptr, 0, st);
-    if (e == hipSuccess) e = launch_pack(dtype, w, o.wp, out, in, o.k.ld, nullptr, 0, st);
+    e = launch_pack2(dtype, x, o.xp, rows, w, o.wp, out, in, o.k.ld, st);
     x = o.xp;
     w = o.wp;
   }
@@ -285,13 +284,10 @@ int singa_linear_bwd(singa_dtype dtype, int rows, int in, int out, const void* x
   if (e == hipSuccess && db)
     e = launch_colsum(o.colsum, db, up(rows, COLSUM_ROWS) / COLSUM_ROWS, out, accumulate, nullptr, st);
   const void* dz = o.own_dz ? o.dz : dy;
-  if (o.k.copy && dx && e == hipSuccess) {
-    e = launch_pack(dtype, w, o.wp, out, in, o.k.ld, nullptr, 0, st);
-    w = o.wp;
-  }
-  if (o.k.copy && dw && e == hipSuccess) {
-    e = launch_pack(dtype, x, o.xp, rows, in, o.k.ld, nullptr, 0, st);
+  if (o.k.copy && (dx || dw) && e == hipSuccess) {
+    e = launch_pack2(dtype, x, o.xp, dw ? rows : 0, w, o.wp, dx ? out : 0, in, o.k.ld, st);
     x = o.xp;
+    w = o.wp;
   }
   Product p;
   p.dt = dtype;
@@ -363,11 +359,8 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
   carve_loss(dtype, rows, in, classes, grad, dw_dtype, ws, &o);
   const void *xt = x, *wt = w;  // as the tiles take them
   if (o.wp) {
-    e = launch_pack(dtype, w, o.wp, classes, in, o.k.ld, nullptr, 0, st);
+    e = launch_pack2(dtype, x, o.xp, rows, w, o.wp, classes, in, o.k.ld, st);
     wt = o.wp;
-  }
-  if (o.xp && e == hipSuccess) {
-    e = launch_pack(dtype, x, o.xp, rows, in, o.k.ld, nullptr, 0, st);
     xt = o.xp;
   }
   Product p;

@@ -145,14 +145,21 @@ template <typename T> hipError_t skinny_t(const Product& p, hipStream_t st) {
 
 // ------------------------------------------------------------ operands
 template <typename T>
-__global__ __launch_bounds__(256) void pack_kernel(const T* __restrict__ in, T* __restrict__ out, long rows, int cols,
+__global__ __launch_bounds__(256) void pack_kernel(const T* __restrict__ in, T* __restrict__ out, long rows,
+                                                   const T* __restrict__ in2, T* __restrict__ out2, long rows2, int cols,
                                                    long ldo, const int32_t* __restrict__ labels, int classes) {
   constexpr int VEC = TypeInfo<T>::VEC;
   const long cpr = ldo / VEC;
   const long i = (long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= rows * cpr) return;
-  const long row = i / cpr;
-  const int c = (int)(i - row * cpr) * VEC;
+  if (i >= (rows + rows2) * cpr) return;
+  long row = i / cpr;
+  const long at = i - row * cpr;
+  if (row >= rows) {
+    row -= rows;
+    in = in2;
+    out = out2;
+  }
+  const int c = (int)at * VEC;
   union { uint4 u; T e[VEC]; } v;
   v.u = make_uint4(0, 0, 0, 0);
   if (!labels || label_ok(labels[row], classes)) {
@@ -512,16 +519,28 @@ hipError_t launch_zero(void* p, size_t bytes, hipStream_t st) {
 
 hipError_t launch_skinny(const Product& p, hipStream_t st) { return p.dt == BF16 ? skinny_t<bf16_t>(p, st) : skinny_t<float>(p, st); }
 
+static hipError_t pack(int dt, const void* in, void* out, long rows, const void* in2, void* out2, long rows2, int cols,
+                       long ldo, const int32_t* labels, int classes, hipStream_t st) {
+  TraceScope ts("pack_kernel", st, (double)(rows + rows2) * (cols + ldo) * dt_size(dt), WORK_BYTE);
+  const long chunks = (rows + rows2) * (ldo / (dt == BF16 ? 8 : 4));
+  const dim3 grid((unsigned)((chunks + 255) / 256));
+  if (dt == BF16)
+    hipLaunchKernelGGL(pack_kernel<bf16_t>, grid, dim3(256), 0, st, (const bf16_t*)in, (bf16_t*)out, rows, (const bf16_t*)in2,
+                       (bf16_t*)out2, rows2, cols, ldo, labels, classes);
+  else
+    hipLaunchKernelGGL(pack_kernel<float>, grid, dim3(256), 0, st, (const float*)in, (float*)out, rows, (const float*)in2,
+                       (float*)out2, rows2, cols, ldo, labels, classes);
+  return hipGetLastError();
+}
+
 hipError_t launch_pack(int dt, const void* in, void* out, long rows, int cols, long ldo, const int32_t* labels, int classes,
                        hipStream_t st) {
-  TraceScope ts("pack_kernel", st, (double)rows * (cols + ldo) * dt_size(dt), WORK_BYTE);
-  if (dt == BF16)
-    hipLaunchKernelGGL(pack_kernel<bf16_t>, dim3((unsigned)((rows * (ldo / 8) + 255) / 256)), dim3(256), 0, st,
-                       (const bf16_t*)in, (bf16_t*)out, rows, cols, ldo, labels, classes);
-  else
-    hipLaunchKernelGGL(pack_kernel<float>, dim3((unsigned)((rows * (ldo / 4) + 255) / 256)), dim3(256), 0, st,
-                       (const float*)in, (float*)out, rows, cols, ldo, labels, classes);
-  return hipGetLastError();
+  return pack(dt, in, out, rows, nullptr, nullptr, 0, cols, ldo, labels, classes, st);
+}
+
+hipError_t launch_pack2(int dt, const void* in, void* out, long rows, const void* in2, void* out2, long rows2, int cols,
+                        long ldo, hipStream_t st) {
+  return pack(dt, in, out, rows, in2, out2, rows2, cols, ldo, nullptr, 0, st);
 }
 
 hipError_t launch_dact(int dt, int act, const void* dy, const void* z, void* dz, void* more, float* colsum, long rows,

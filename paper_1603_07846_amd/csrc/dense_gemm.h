@@ -83,9 +83,16 @@ template <typename T> __device__ __forceinline__ float act_f(float z, int act) {
 // act'(z): dz = dy act'(z)
 template <typename T> __device__ __forceinline__ float act_slope(float z, int act) {
   if (act == ACT_RELU) return z > 0.f ? 1.f : 0.f;
-  if (act == ACT_GELU) return fmaf(z * 0.39894228040143268f, expf(-0.5f * z * z), 0.5f * erfcf(-z * 0.70710678118654752f));
+  constexpr bool FAST = sizeof(T) == 2;  // 1.5e-7 off at most, below dz's own rounding
+  if (act == ACT_GELU) {
+    if constexpr (FAST) {  // one exponential serves both terms
+      const float u = fabsf(z) * 0.70710678118654752f, e = exp_fast(-u * u), h = 0.5f * erfc_poly(u) * e;
+      return fmaf(z * 0.39894228040143268f, e, z < 0.f ? h : 1.f - h);
+    }
+    return fmaf(z * 0.39894228040143268f, expf(-0.5f * z * z), 0.5f * erfcf(-z * 0.70710678118654752f));
+  }
   if (act == ACT_SILU) {
-    const float s = 1.f / (1.f + expf(-z));
+    const float s = FAST ? __builtin_amdgcn_rcpf(1.f + exp_fast(-z)) : 1.f / (1.f + expf(-z));
     return s * fmaf(z, 1.f - s, 1.f);
   }
   return 1.f;
@@ -115,6 +122,16 @@ template <> __device__ __forceinline__ void store8<float>(float* p, const float 
 template <> __device__ __forceinline__ void store8<bf16_t>(bf16_t* p, const float (&v)[8]) {
   *(u32x4_t*)p = u32x4_t{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]),
                          f32x2_to_bf16x2(v[6], v[7])};
+}
+
+// The value of lane l ^ d for d = 1, 2; for d = 4 that of the lane mirrored in
+// its group of 8, which holds the same once groups of 4 agree.  Data-parallel
+// moves, no LDS round trip.
+__device__ __forceinline__ float lane_xor(float v, int d) {
+  const int x = __float_as_int(v);
+  return __int_as_float(d == 1   ? __builtin_amdgcn_update_dpp(0, x, 0xb1, 0xf, 0xf, true)   // quad_perm [1,0,3,2]
+                        : d == 2 ? __builtin_amdgcn_update_dpp(0, x, 0x4e, 0xf, 0xf, true)   // quad_perm [2,3,0,1]
+                                 : __builtin_amdgcn_update_dpp(0, x, 0x141, 0xf, 0xf, true));  // row_half_mirror
 }
 
 // v at y + o and, with more, its further terms, `step` elements apart.
@@ -199,22 +216,20 @@ template <typename T, int n> __device__ __forceinline__ void act_all(float (&v)[
   }
 }
 
-// EPI_OUT on 8 columns from col of R rows `step` apart, in 16-byte vectors
-// (N % 8 == 0 and every tensor starts at a 16-byte boundary).  x: what is
-// added (e.res or e.add); live: false where a label takes the row out.
-template <typename T, int R>
-__device__ __forceinline__ void epi_out(const Epilogue& e, int M, int N, int row0, int step, int col, float (&v)[R][8],
-                                        const Columns& c, const Extra (&x)[R], const bool (&live)[R]) {
+// EPI_OUT on 8 columns of R rows, in 16-byte vectors (N % 8 == 0 and every
+// tensor starts at a 16-byte boundary).  x: what is added (e.res or e.add);
+// live: false where a label takes the row out; put_z, put_y: store row u;
+// before_y: what goes between the last use of x and the stores.
+template <typename T, int R, typename PutZ, typename PutY, typename Before>
+__device__ __forceinline__ void epi_out(const Epilogue& e, float (&v)[R][8], const Columns& c, const Extra (&x)[R],
+                                        const bool (&live)[R], PutZ put_z, PutY put_y, Before before_y) {
 #pragma unroll
   for (int u = 0; u < R; ++u)
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[u][j] = fmaf(v[u][j], c.alpha, c.bias[j]);
   if (e.z) {
 #pragma unroll
-    for (int u = 0; u < R; ++u) {
-      const int row = row0 + u * step;
-      if (row < M && col < N) store8<T>((T*)e.z + (size_t)row * N + col, v[u]);
-    }
+    for (int u = 0; u < R; ++u) put_z(u, v[u]);
   }
   if (e.act) {
 #pragma unroll
@@ -230,16 +245,23 @@ __device__ __forceinline__ void epi_out(const Epilogue& e, int M, int N, int row
 #pragma unroll
     for (int u = 0; u < R; ++u) add_extra<T>(e.add, x[u], v[u]);
   }
+  before_y();
 #pragma unroll
-  for (int u = 0; u < R; ++u) {
-    const int row = row0 + u * step;
-    const size_t o = (size_t)row * e.ldy + col;
-    if (row < M && col < N) {
-      if (e.out_f32)
-        store8<float>((float*)e.y + o, v[u]);
-      else
-        store8<T>((T*)e.y + o, v[u]);
-    }
+  for (int u = 0; u < R; ++u) put_y(u, v[u]);
+}
+
+// 8 values at byte offset o of a buffer (past its end: not stored, and no
+// branch that the stores around it would have to be counted across)
+template <typename T> __device__ __forceinline__ void buf_store8(__amdgpu_buffer_rsrc_t r, uint32_t o, const float (&v)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    const u32x4_t p = {f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]),
+                       f32x2_to_bf16x2(v[6], v[7])};
+    __builtin_amdgcn_raw_buffer_store_b128(p, r, (int)o, 0, 0);
+  } else {
+    const u32x4_t lo = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    const u32x4_t hi = {__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
+    __builtin_amdgcn_raw_buffer_store_b128(lo, r, (int)o, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(hi, r, (int)o, 16, 0);
   }
 }
 
@@ -576,7 +598,7 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(G
   // Stores count as outstanding like loads, and a wait for a load waits for
   // every store before it: so what the rows take besides their sums is loaded
   // before the first store (the rows' labels and lse go through LDS), and what
-  // is added to them a whole block at a time.
+  // is added to them a whole block ahead.
   struct RowInfo {
     int lab;
     float lse;
@@ -603,21 +625,28 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(G
 #pragma unroll
       for (int v = 0; v < 16; ++v) q[(8 * (v >> 2) + 4 * lh + (v & 3)) * PIT + bn * 16 + wcol] = acc[bm][bn][v];
   };
+  Extra extra[UN];
+  const bool adds = EPI == EPI_OUT && g.vec && !g.raw && (g.e.res || g.e.add);
+  auto load_block = [&](int bm) {
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int row = m0 + (wm * FM + bm) * 32 + u * RPP + rr;
+      extra[u] = load_extra<T>(g.e, g.N, row, col, row < g.M && col < g.N);
+    }
+  };
+  // y and z from the tile's first row on: 32-bit offsets
+  auto rows_from = [&](const void* p, long ld, int es) {
+    const long left = ((long)g.M - m0) * ld * es;
+    return make_rsrc((const char*)p + (long)m0 * ld * es, left > 0x7ffffff0L ? 0x7ffffff0u : (uint32_t)left);
+  };
+  const int ys = g.e.out_f32 ? 4 : (int)sizeof(T);
+  __amdgpu_buffer_rsrc_t yr = rows_from(g.e.y, g.e.ldy, ys), zr = rows_from(g.e.z, g.N, (int)sizeof(T));
+  if (adds) load_block(0);
   // The accumulators' registers need constant indexes, the rest does not: one
   // copy of it, which stays in the instruction cache.
 #pragma unroll 1
   for (int bm = 0; bm < FM; ++bm) {
     const int row0 = m0 + (wm * FM + bm) * 32;
-    Extra extra[UN];
-    if constexpr (EPI == EPI_OUT) {
-      if (g.vec && !g.raw && (g.e.res || g.e.add)) {
-#pragma unroll
-        for (int u = 0; u < UN; ++u) {
-          const int row = row0 + u * RPP + rr;
-          extra[u] = load_extra<T>(g.e, g.N, row, col, row < g.M && col < g.N);
-        }
-      }
-    }
     if (bm == 0) stage_block(Const<0>{});
     if (bm == 1) stage_block(Const<1>{});
     if constexpr (FM == 4) {
@@ -645,7 +674,22 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(G
           read(r, v[u]);
           live[u] = !rows_have || label_ok(info[row0 + r - m0].lab, g.e.classes);
         }
-        epi_out<T, UN>(g.e, g.M, g.N, row0 + rr, RPP, col, v, cols, extra, live);
+        auto at = [&](int u, long ld, int es) {
+          const int r = row0 - m0 + u * RPP + rr;
+          return m0 + r < g.M && col < g.N ? (uint32_t)(((long)r * ld + col) * es) : OOB;
+        };
+        epi_out<T, UN>(
+            g.e, v, cols, extra, live, [&](int u, const float(&w)[8]) { buf_store8<T>(zr, at(u, g.N, (int)sizeof(T)), w); },
+            [&](int u, const float(&w)[8]) {
+              if (g.e.out_f32)
+                buf_store8<float>(yr, at(u, g.e.ldy, 4), w);
+              else
+                buf_store8<T>(yr, at(u, g.e.ldy, (int)sizeof(T)), w);
+            },
+            // the next block's before this one's stores, which its wait then leaves alone
+            [&] {
+              if (adds && bm + 1 < FM) load_block(bm + 1);
+            });
       } else {
 #pragma unroll 1
         for (int u = 0; u < UN; ++u) {
@@ -682,13 +726,13 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(G
           }
           float m = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
 #pragma unroll
-          for (int d = 1; d < LPG; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+          for (int d = 1; d < LPG; d <<= 1) m = fmaxf(m, lane_xor(m, d));
           const float ms = m == -INFINITY ? 0.f : m;
           float s = 0.f;  // NaN where a value is (fmaxf passed over it)
 #pragma unroll
           for (int j = 0; j < 8; ++j) s += exp_fast(v[j] - ms);
 #pragma unroll
-          for (int d = 1; d < LPG; d <<= 1) s += __shfl_xor(s, d);
+          for (int d = 1; d < LPG; d <<= 1) s += lane_xor(s, d);
           if (row < g.M) {
             if (c8 % STAT_COLS == 0 && col < g.N)
               g.e.stats[(size_t)row * g.e.nstat + g.e.stat0 + col / STAT_COLS] = make_float2(m, s);
@@ -749,11 +793,14 @@ template <typename T> __global__ __launch_bounds__(256) void product_reduce_kern
   const float* p = g.partial + (size_t)row * g.ldp + col;
   const size_t step = (size_t)g.M * g.ldp;
   load8<float>(p, v);
-  for (int s = 1; s < g.splits; ++s) {
-    float u[8];
-    load8<float>(p + s * step, u);
+  for (int s = 1; s < g.splits; s += 4) {  // four loads under way, added in order
+    float u[4][8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] += u[j];
+    for (int i = 0; i < 4; ++i) load8<float>(p + min(s + i, g.splits - 1) * step, u[i]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += s + i < g.splits ? u[i][j] : 0.f;
   }
   const bool live = !g.e.labels || label_ok(g.e.labels[row], g.e.classes);
   const Columns c = columns_of(g.e, g.N, col);
@@ -763,33 +810,53 @@ template <typename T> __global__ __launch_bounds__(256) void product_reduce_kern
   if (g.e.res || g.e.add) x[0] = load_extra<T>(g.e, g.N, row, col, true);
 #pragma unroll
   for (int j = 0; j < 8; ++j) v1[0][j] = v[j];
-  epi_out<T, 1>(g.e, g.M, g.N, row, 0, col, v1, c, x, {live});
+  const size_t o = (size_t)row * g.N + col, oy = (size_t)row * g.e.ldy + col;
+  epi_out<T, 1>(
+      g.e, v1, c, x, {live}, [&](int, const float(&w)[8]) { store8<T>((T*)g.e.z + o, w); },
+      [&](int, const float(&w)[8]) {
+        if (g.e.out_f32)
+          store8<float>((float*)g.e.y + oy, w);
+        else
+          store8<T>((T*)g.e.y + oy, w);
+      },
+      [] {});
 }
 
 struct Plan {
   int big, splits, kt_split;
 };
 
-// 256 x 256 tiles (bf16) where they fill most of the chip; otherwise 128 x 128
-// ones, and, where those are fewer than the workgroups that run at once, the K
-// range cut so that about 512 run, each with at least 8 K-tiles.
+// The tile and the cut of the K range, from a model of the time in us that
+// follows what was measured (MI355X, 24 products of 128 .. 4096 rows, 256 ..
+// 32768 of k): a K-tile takes 1.42 in a 256 x 256 tile (bf16, one workgroup
+// per CU, 10 more per tile); in a 128 x 128 tile 0.44 (fp32 1.95) while there
+// is one workgroup per CU and 1.0 (3.9) at two, 5 more per tile; a cut costs
+// the second launch, 4, and its partial sums' bytes at some 6 TB/s.
 inline Plan plan_product(int dt, int M, int N, int K, int epi) {
   auto up = [](long a, long b) { return (a + b - 1) / b; };
-  const int bk = dt == BF16 ? 64 : 32;
-  const int kt = (int)up(K, bk);
+  const int kt = (int)up(K, dt == BF16 ? 64 : 32);
   Plan p{0, 1, kt};
-  if (dt == BF16 && up(M, 256) * up(N, 256) >= 192) {
-    p.big = 1;
-    return p;
-  }
-  const long tiles = up(M, 128) * up(N, 128);
-  if (epi == EPI_OUT && tiles < 256) {
-    long s = 512 / tiles;
-    if (s > kt / 8) s = kt / 8;
-    if (s > 32) s = 32;
-    if (s > 1) {
-      p.kt_split = (int)up(kt, s);
-      p.splits = (int)up(kt, p.kt_split);
+  double best = 1e30;
+  for (int big = 0; big < (dt == BF16 ? 2 : 1); ++big) {
+    const long tiles = big ? up(M, 256) * up(N, 256) : up(M, 128) * up(N, 128);
+    for (int s = 1; s <= 32 && s <= kt && (s == 1 || epi == EPI_OUT); ++s) {
+      const long n = tiles * s;
+      if (s > 1 && n > 512) break;
+      const long per = up(kt, s);
+      double t;
+      if (big)
+        t = (double)up(n, 256) * (per * 1.42 + 10);
+      else if (dt == BF16)
+        t = (double)up(n, 512) * (per * (n <= 256 ? 0.44 : n >= 512 ? 1.0 : 0.44 + (n - 256) / 256.0 * 0.56) + 5);
+      else
+        t = (double)up(n, 256) * per * 1.95 + (double)up(n, 512) * 5;
+      if (s > 1) t += 4 + s * (double)M * N * 8 / 6e6;
+      if (t < best) {
+        best = t;
+        p.big = big;
+        p.kt_split = (int)per;
+        p.splits = (int)up(kt, per);
+      }
     }
   }
   return p;
