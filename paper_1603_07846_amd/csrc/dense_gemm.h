@@ -156,11 +156,14 @@ __device__ __forceinline__ bool label_ok(int lab, int classes) { return lab >= 0
 struct Columns {
   float alpha, bias[8];
 };
-__device__ __forceinline__ Columns columns_of(const Epilogue& e, int N, int col) {
+__device__ __forceinline__ Columns columns_of(const Epilogue& e, int N, int col, int colb) {
   Columns c;
   c.alpha = e.alpha ? e.alpha[0] : 1.f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) c.bias[j] = e.bias && col + j < N ? e.bias[col + j] : 0.f;
+  for (int j = 0; j < 8; ++j) {
+    const int k = j < 4 ? col + j : colb + j - 4;
+    c.bias[j] = e.bias && k < N ? e.bias[k] : 0.f;
+  }
   return c;
 }
 
@@ -169,18 +172,20 @@ __device__ __forceinline__ Columns columns_of(const Epilogue& e, int N, int col)
 struct Extra {
   uint4 a, b;
 };
-template <typename T> __device__ __forceinline__ Extra load_extra(const Epilogue& e, int N, int row, int col, bool in) {
+template <typename T>
+__device__ __forceinline__ Extra load_extra(const Epilogue& e, int M, int N, int row, int col, int colb) {
   // every lane reads (element 0 stands in for what lies outside), so that no
   // load sits in a branch that the next one waits for
   Extra x;
+  const bool in = row < M && col < N, inb = row < M && colb < N;
   if (e.add) {
-    const float* p = (const float*)e.y + (in ? (size_t)row * e.ldy + col : 0);
-    x.a = *(const uint4*)p;
-    x.b = *(const uint4*)(p + 4);
+    const float* p = (const float*)e.y;
+    x.a = *(const uint4*)(p + (in ? (size_t)row * e.ldy + col : 0));
+    x.b = *(const uint4*)(p + (inb ? (size_t)row * e.ldy + colb : 0));
   } else {
-    const T* p = (const T*)e.res + (in ? (size_t)row * N + col : 0);
-    x.a = *(const uint4*)p;
-    x.b = sizeof(T) == 4 ? *(const uint4*)(p + 4) : x.a;
+    const T* p = (const T*)e.res;
+    x.a = *(const uint4*)(p + (in ? (size_t)row * N + col : 0));
+    x.b = sizeof(T) == 4 ? *(const uint4*)(p + (inb ? (size_t)row * N + colb : 0)) : x.a;
   }
   return x;
 }
@@ -250,39 +255,39 @@ __device__ __forceinline__ void epi_out(const Epilogue& e, float (&v)[R][8], con
   for (int u = 0; u < R; ++u) put_y(u, v[u]);
 }
 
-// 8 values at byte offset o of a buffer (past its end: not stored, and no
-// branch that the stores around it would have to be counted across)
-template <typename T> __device__ __forceinline__ void buf_store8(__amdgpu_buffer_rsrc_t r, uint32_t o, const float (&v)[8]) {
-  if constexpr (sizeof(T) == 2) {
-    const u32x4_t p = {f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]),
-                       f32x2_to_bf16x2(v[6], v[7])};
-    __builtin_amdgcn_raw_buffer_store_b128(p, r, (int)o, 0, 0);
-  } else {
-    const u32x4_t lo = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-    const u32x4_t hi = {__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
-    __builtin_amdgcn_raw_buffer_store_b128(lo, r, (int)o, 0, 0);
-    __builtin_amdgcn_raw_buffer_store_b128(hi, r, (int)o, 16, 0);
-  }
+// Four fp32 values, or eight as bf16, at byte offset o of a buffer (past its
+// end: not stored, and no branch that the stores around it would have to be
+// counted across).  NT: non-temporal, for outputs that this launch does not
+// read again (8192^3: 819 -> 810 us).
+template <bool NT> __device__ __forceinline__ void buf_store4(__amdgpu_buffer_rsrc_t r, uint32_t o, const float* v) {
+  const u32x4_t p = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+  __builtin_amdgcn_raw_buffer_store_b128(p, r, (int)o, 0, NT ? 2 : 0);
+}
+template <bool NT> __device__ __forceinline__ void buf_store8h(__amdgpu_buffer_rsrc_t r, uint32_t o, const float (&v)[8]) {
+  const u32x4_t p = {f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]),
+                     f32x2_to_bf16x2(v[6], v[7])};
+  __builtin_amdgcn_raw_buffer_store_b128(p, r, (int)o, 0, NT ? 2 : 0);
 }
 
 // The same, element by element, for any N.
 template <typename T>
-__device__ __forceinline__ void epi_out_any(const Epilogue& e, int N, int row, int col, const float (&v)[8], const Columns& c,
-                                            bool live) {
-  const size_t o = (size_t)row * N + col, oy = (size_t)row * e.ldy + col;
+__device__ __forceinline__ void epi_out_any(const Epilogue& e, int N, int row, int col, int colb, const float (&v)[8],
+                                            const Columns& c, bool live) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    if (col + j >= N) break;
+    const int k = j < 4 ? col + j : colb + j - 4;
+    if (k >= N) continue;
+    const size_t o = (size_t)row * N + k, oy = (size_t)row * e.ldy + k;
     float y = fmaf(v[j], c.alpha, c.bias[j]);
-    if (e.z) store_out<T>((T*)e.z + o + j, y);
+    if (e.z) store_out<T>((T*)e.z + o, y);
     if (e.act) y = act_f<T>(y, e.act);
     if (!live) y = 0.f;
-    if (e.res) y += elem_f(((const T*)e.res)[o + j]);
-    if (e.add) y += ((const float*)e.y)[oy + j];
+    if (e.res) y += elem_f(((const T*)e.res)[o]);
+    if (e.add) y += ((const float*)e.y)[oy];
     if (e.out_f32)
-      ((float*)e.y)[oy + j] = y;
+      ((float*)e.y)[oy] = y;
     else
-      store_out<T>((T*)e.y + oy + j, y);
+      store_out<T>((T*)e.y + oy, y);
   }
 }
 
@@ -574,19 +579,24 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(G
   constexpr int RPP = 64 / LPR;  // rows per pass
   constexpr int UN = 32 / RPP;   // passes of a block
   const int li = lane & 31, lh = lane >> 5;
-  const int c8 = (lane % LPR) * 8, rr = lane / LPR;
-  const int col = n0 + wn * FN * 32 + c8;
+  const int lr = lane % LPR, c8 = lr * 8, rr = lane / LPR;
+  // A lane's columns: col .. col + 3 and colb .. colb + 3.  What is stored as
+  // bf16 takes eight in a row; fp32 stores take four of each half of the wave's
+  // columns, so that each instruction writes whole lines.
+  const bool wide = EPI == EPI_OUT && (sizeof(T) == 4 || g.e.out_f32 || g.raw);
+  const int col = n0 + wn * FN * 32 + (wide ? lr * 4 : c8), colb = wide ? col + FN * 16 : col + 4;
+  const int qa = wide ? (lr >> 1) * 4 + (lr & 1 ? HALF : 0) : c8 / 2, qb = wide ? qa + FN * 8 : qa + HALF;
   const int wcol = (li & 3) + ((li >> 3) << 2) + (li & 4 ? HALF : 0);
   auto read = [&](int r, float (&v)[8]) {
-    const float* s = q + r * PIT + c8 / 2;
-    const f32x4 a = *(const f32x4*)s, b = *(const f32x4*)(s + HALF);
+    const float* s = q + r * PIT;
+    const f32x4 a = *(const f32x4*)(s + qa), b = *(const f32x4*)(s + qb);
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = a[j], v[4 + j] = b[j];
   };
   Columns cols{};
   float cs[8];
   if constexpr (EPI == EPI_OUT) {
-    cols = columns_of(g.e, g.N, col);
+    cols = columns_of(g.e, g.N, col, colb);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -631,16 +641,33 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(G
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
       const int row = m0 + (wm * FM + bm) * 32 + u * RPP + rr;
-      extra[u] = load_extra<T>(g.e, g.N, row, col, row < g.M && col < g.N);
+      extra[u] = load_extra<T>(g.e, g.M, g.N, row, col, colb);
     }
   };
-  // y and z from the tile's first row on: 32-bit offsets
-  auto rows_from = [&](const void* p, long ld, int es) {
-    const long left = ((long)g.M - m0) * ld * es;
-    return make_rsrc((const char*)p + (long)m0 * ld * es, left > 0x7ffffff0L ? 0x7ffffff0u : (uint32_t)left);
+  // Outputs from the tile's first row on, with 32-bit offsets: a lane's place in
+  // the block's first row, computed once, and the rows' steps in scalar
+  // registers.  Rows past the end lie past the buffer's, columns past it OOB.
+  auto rows_from = [&](const void* p, long rows, uint32_t pitch) {
+    const long left = (rows - m0) * pitch;
+    return make_rsrc((const char*)p + (long)m0 * pitch, left > 0x7ffffff0L ? 0x7ffffff0u : left > 0 ? (uint32_t)left : 0u);
+  };
+  auto place = [&](int c, int cols, uint32_t pitch, int es) {
+    return c < cols ? (uint32_t)(wm * FM * 32 + rr) * pitch + (uint32_t)(c * es) : OOB;
   };
   const int ys = g.e.out_f32 ? 4 : (int)sizeof(T);
-  __amdgpu_buffer_rsrc_t yr = rows_from(g.e.y, g.e.ldy, ys), zr = rows_from(g.e.z, g.N, (int)sizeof(T));
+  const uint32_t pitch_y = (uint32_t)g.e.ldy * ys, pitch_z = (uint32_t)g.N * (int)sizeof(T), pitch_p = (uint32_t)g.ldp * 4;
+  const __amdgpu_buffer_rsrc_t yr = rows_from(g.e.y, EPI == EPI_DLOGITS ? g.e.rows_padded : g.M, pitch_y),
+                               zr = rows_from(g.e.z, g.M, pitch_z),
+                               pr = rows_from(g.partial + (size_t)split * g.M * g.ldp, g.M, pitch_p);
+  const uint32_t at_y = place(col, EPI == EPI_DLOGITS ? (int)g.e.ldy : g.N, pitch_y, ys), at_yb = place(colb, g.N, pitch_y, ys),
+                 at_z = place(col, g.N, pitch_z, (int)sizeof(T)), at_zb = place(colb, g.N, pitch_z, (int)sizeof(T)),
+                 at_p = place(col, g.N, pitch_p, 4), at_pb = place(colb, g.N, pitch_p, 4);
+  __amdgpu_buffer_rsrc_t mr0 = yr, mr1 = yr;  // the further terms
+  if (EPI == EPI_DLOGITS && g.e.more) {
+    static_assert(TERMS == 3, "two further terms");
+    mr0 = rows_from(g.e.more, g.e.rows_padded, pitch_y);
+    mr1 = rows_from(g.e.more + (size_t)g.e.rows_padded * g.e.ldy, g.e.rows_padded, pitch_y);
+  }
   if (adds) load_block(0);
   // The accumulators' registers need constant indexes, the rest does not: one
   // copy of it, which stays in the instruction cache.
@@ -662,8 +689,9 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(G
         for (int u = 0; u < UN; ++u) read(u * RPP + rr, v[u]);
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
-          const int row = row0 + u * RPP + rr;
-          if (row < g.M && col < g.N) store8<float>(g.partial + ((size_t)split * g.M + row) * g.ldp + col, v[u]);
+          const uint32_t step = (uint32_t)(bm * 32 + u * RPP) * pitch_p;
+          buf_store4<false>(pr, at_p + step, v[u]);
+          buf_store4<false>(pr, at_pb + step, v[u] + 4);
         }
       } else if (g.vec) {
         float v[UN][8];
@@ -674,18 +702,18 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(G
           read(r, v[u]);
           live[u] = !rows_have || label_ok(info[row0 + r - m0].lab, g.e.classes);
         }
-        auto at = [&](int u, long ld, int es) {
-          const int r = row0 - m0 + u * RPP + rr;
-          return m0 + r < g.M && col < g.N ? (uint32_t)(((long)r * ld + col) * es) : OOB;
+        auto put = [&](__amdgpu_buffer_rsrc_t b, uint32_t o, uint32_t ob, uint32_t pitch, int u, const float(&w)[8]) {
+          const uint32_t step = (uint32_t)(bm * 32 + u * RPP) * pitch;
+          if (wide) {
+            buf_store4<true>(b, o + step, w);
+            buf_store4<true>(b, ob + step, w + 4);
+          } else {
+            buf_store8h<true>(b, o + step, w);
+          }
         };
         epi_out<T, UN>(
-            g.e, v, cols, extra, live, [&](int u, const float(&w)[8]) { buf_store8<T>(zr, at(u, g.N, (int)sizeof(T)), w); },
-            [&](int u, const float(&w)[8]) {
-              if (g.e.out_f32)
-                buf_store8<float>(yr, at(u, g.e.ldy, 4), w);
-              else
-                buf_store8<T>(yr, at(u, g.e.ldy, (int)sizeof(T)), w);
-            },
+            g.e, v, cols, extra, live, [&](int u, const float(&w)[8]) { put(zr, at_z, at_zb, pitch_z, u, w); },
+            [&](int u, const float(&w)[8]) { put(yr, at_y, at_yb, pitch_y, u, w); },
             // the next block's before this one's stores, which its wait then leaves alone
             [&] {
               if (adds && bm + 1 < FM) load_block(bm + 1);
@@ -697,7 +725,7 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(G
           const bool live = !rows_have || label_ok(info[row - m0].lab, g.e.classes);
           float v[8];
           read(r, v);
-          if (row < g.M && col < g.N) epi_out_any<T>(g.e, g.N, row, col, v, cols, live);
+          if (row < g.M) epi_out_any<T>(g.e, g.N, row, col, colb, v, cols, live);
         }
       }
     } else {
@@ -756,8 +784,21 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(G
           }
 #pragma unroll
           for (int j = 0; j < 8; ++j) cs[j] += v[j];
-          if (row < g.e.rows_padded && col < g.e.ldy)
-            store_terms<T>((T*)g.e.y, g.e.more, (size_t)row * g.e.ldy + col, (size_t)g.e.rows_padded * g.e.ldy, v);
+          const uint32_t o = at_y + (uint32_t)(bm * 32 + u * RPP) * pitch_y;
+          if constexpr (sizeof(T) == 4) {
+            buf_store4<false>(yr, o, v);
+            buf_store4<false>(yr, o + 16, v + 4);
+          } else {
+            buf_store8h<false>(yr, o, v);
+            if (g.e.more) {
+#pragma unroll
+              for (int t = 0; t < TERMS - 1; ++t) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] -= bf16_to_f32(f32_to_bf16(v[j]));
+                buf_store8h<false>(t ? mr1 : mr0, o, v);
+              }
+            }
+          }
         }
       }
     }
@@ -803,11 +844,11 @@ template <typename T> __global__ __launch_bounds__(256) void product_reduce_kern
       for (int j = 0; j < 8; ++j) v[j] += s + i < g.splits ? u[i][j] : 0.f;
   }
   const bool live = !g.e.labels || label_ok(g.e.labels[row], g.e.classes);
-  const Columns c = columns_of(g.e, g.N, col);
-  if (!g.vec) return epi_out_any<T>(g.e, g.N, row, col, v, c, live);
+  const Columns c = columns_of(g.e, g.N, col, col + 4);
+  if (!g.vec) return epi_out_any<T>(g.e, g.N, row, col, col + 4, v, c, live);
   Extra x[1];
   float v1[1][8];
-  if (g.e.res || g.e.add) x[0] = load_extra<T>(g.e, g.N, row, col, true);
+  if (g.e.res || g.e.add) x[0] = load_extra<T>(g.e, g.M, g.N, row, col, col + 4);
 #pragma unroll
   for (int j = 0; j < 8; ++j) v1[0][j] = v[j];
   const size_t o = (size_t)row * g.N + col, oy = (size_t)row * g.e.ldy + col;

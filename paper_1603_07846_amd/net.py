@@ -34,6 +34,12 @@ With ``concurrent_wgrad`` (the default on a GPU) the filter gradients, and
 the fused gradient + update of the fully connected layers, run on a second
 stream as soon as their inputs exist, beside the backward-data passes of the
 layers below; the backward loop ends by joining the two streams.
+
+With ``fused_loss`` the last fully connected layer and the softmax loss run as
+one call that does not keep the logits (singa.linear_softmax_ce): the layer
+passes its input on, and the loss layer leaves the loss and the layer's
+gradients.  With ``clip_norm`` the update is preceded by the global norm of all
+gradients and takes its clipping scale from device memory.
 """
 from __future__ import annotations
 
@@ -83,6 +89,7 @@ class ConvLayer(Layer):
         self.relu = False  # set when a ReLU layer directly follows and is fused
         self.relu_src = None  # the ReLU layer feeding this one, whose backward bwd-data folds in
         self.event = None  # see _fork
+        self.head = False  # carried out by the loss layer (Net's fused_loss)
         dev, dt = net.device, net.dtype
         # update fused into the filter-gradient kernel (no workspace needed exactly then)
         self.fused_update = bool(net.fuse_update and net.wl.update and net.updater == "sgd" and singa.conv_workspace_bytes(
@@ -119,6 +126,9 @@ class ConvLayer(Layer):
         self.v, self.vb, self.b_compute = v, vb, b_compute
 
     def compute_feature(self, x):
+        if self.head:
+            self.x = x
+            return x
         if self.xs is not None:
             singa.space_to_depth(x, self.w_shape, self.pad, self.stride, out=self.xs)
             x = self.xs
@@ -128,6 +138,8 @@ class ConvLayer(Layer):
         return self.y
 
     def compute_gradient(self, dy, need_dx=True):
+        if self.head:
+            return dy  # the loss layer formed this layer's gradients, dy is the one at its input
         if self.fused_update or self.reduce_update:
             # backward-data first: it reads the bf16 weights the update rewrites
             # (fused into the gradient kernel, or applied by its split-K
@@ -270,13 +282,41 @@ class SoftmaxCELayer(Layer):
         return self.dz
 
 
+class FusedLossLayer(Layer):
+    """The softmax loss of a fully connected layer's output without its logits;
+    the gradients of that layer come with it.  A row whose label is outside
+    [0, classes) is padding here."""
+
+    def __init__(self, net, spec, fc: ConvLayer):
+        self.name = spec.name
+        self.fc = fc
+        fc.head = True
+        fc.fused_update = fc.reduce_update = False
+        B, n = fc.in_shape[0], int(np.prod(fc.in_shape[1:]))
+        self.flat = (B, n)
+        self.loss = singa.empty((B + 1,), torch.float32, net.device)  # mean, then rows
+        self.workspace = singa.empty((max(256, singa.linear_softmax_ce_workspace_bytes(net.dtype, B, n, fc.K)),), torch.uint8,
+                                     net.device)
+        self.labels = None
+        self.out_shape = (1,)
+
+    def compute_feature(self, x):
+        fc, n = self.fc, self.flat[1]
+        singa.linear_softmax_ce(x.view(self.flat), fc.w_compute.view(fc.K, n), self.labels, fc.b, loss=self.loss,
+                                dx=fc.dx.view(self.flat), dw=fc.dw.view(fc.K, n), db=fc.db, workspace=self.workspace)
+        return self.loss
+
+    def compute_gradient(self, dy=None, need_dx=True):
+        return self.fc.dx
+
+
 class Net:
     """A workload's layer stack on one GPU, with flat parameter buffers."""
 
     def __init__(self, workload: wl.Workload, batch: Optional[int] = None, device="cuda", fuse_update: bool = True,
                  keep_grads: bool = False, concurrent_wgrad: bool = True, updater: str = "sgd",
                  adagrad_delta: float = 1e-6, reduce_update: bool = False, last_wgrad_on_main: bool = True,
-                 side_update: bool = True):
+                 side_update: bool = True, fused_loss: bool = False, clip_norm: Optional[float] = None):
         """fuse_update: apply the update inside the filter-gradient kernel
         where it can be fused; keep_grads: those layers also store their
         gradients in the flat gradient buffer (for inspection);
@@ -292,7 +332,19 @@ class Net:
         ran there (all but the first) also runs there, once the main stream
         has issued the last backward-data pass that reads those weights,
         beside the first layer's filter gradient on the main stream (0.4-0.6 %
-        faster on the AlexNet-shaped step than the whole update after it)."""
+        faster on the AlexNet-shaped step than the whole update after it);
+        fused_loss: a fully connected layer at the end and its softmax loss
+        run as one call without the logits (the layer's y is not written and
+        its ReLU source is not folded; labels outside the classes are padding
+        rows); clip_norm: every update's gradients are scaled down to this
+        global norm (grad_stat: the norm and the scale of the last update), so
+        none is applied before all are there: no update is fused or runs
+        beside the backward pass."""
+        if clip_norm is not None and not clip_norm >= 0:
+            raise ValueError("clip_norm: %r" % clip_norm)
+        if clip_norm is not None:
+            fuse_update = reduce_update = side_update = False
+        self.clip_norm = clip_norm
         if updater not in ("sgd", "adagrad"):
             raise ValueError(updater)
         self.updater = updater
@@ -312,7 +364,10 @@ class Net:
         C, H, W = workload.in_shape
         shape = (self.batch, H, W, C)
         prev = None
-        for spec in workload.layers:
+        specs = list(workload.layers)
+        fused_loss = fused_loss and len(specs) > 1 and isinstance(specs[-1], wl.SoftmaxCE) and isinstance(specs[-2], wl.FC)
+        for i, spec in enumerate(specs):
+            head = fused_loss and i == len(specs) - 2
             if isinstance(spec, wl.Conv):
                 layer = ConvLayer(self, spec, shape)
             elif isinstance(spec, wl.FC):
@@ -326,13 +381,15 @@ class Net:
                 layer = ReluLayer(self, spec, shape, fuse)
             elif isinstance(spec, wl.Lrn):
                 layer = LrnLayer(self, spec, shape)
+            elif isinstance(spec, wl.SoftmaxCE) and fused_loss:
+                layer = FusedLossLayer(self, spec, prev)
             elif isinstance(spec, wl.SoftmaxCE):
                 layer = SoftmaxCELayer(self, spec, shape)
             else:
                 raise TypeError(spec)
             # a convolution's backward-data or a max pooling's backward can
             # also apply the backward of the ReLU that feeds it
-            if isinstance(prev, ReluLayer) and (isinstance(layer, ConvLayer) or
+            if not head and isinstance(prev, ReluLayer) and (isinstance(layer, ConvLayer) or
                                                (isinstance(layer, PoolLayer) and layer.mode == "max")):
                 layer.relu_src = prev
                 prev.folded = True
@@ -347,6 +404,9 @@ class Net:
         if concurrent_wgrad and self.device.type == "cuda" and any(isinstance(l, ConvLayer) for l in self.layers):
             self.wgrad_stream = torch.cuda.Stream(device=self.device)
             self.workspace_wgrad = singa.empty((max(self.ws_wgrad_bytes, 256),), torch.uint8, self.device)
+        if clip_norm is not None:
+            self.grad_stat = singa.empty((2,), torch.float32, self.device).zero_()
+            self.norm_workspace = singa.empty((singa.grad_norm_workspace_bytes(1),), torch.uint8, self.device)
         self._build_params()
 
     def need_workspace(self, nbytes: int):
@@ -430,7 +490,7 @@ class Net:
     def forward(self, x, labels=None):
         h = x
         for l in self.layers:
-            if isinstance(l, SoftmaxCELayer):
+            if isinstance(l, (SoftmaxCELayer, FusedLossLayer)):
                 l.labels = labels
             h = l.compute_feature(h)
         return h
@@ -462,7 +522,11 @@ class Net:
         filter-gradient kernel, over their parts of the flat buffers; after a
         backward pass with a deferred join, the layers whose filter gradient
         ran on the second stream are updated there (once the main stream has
-        issued their backward-data passes), then the streams join."""
+        issued their backward-data passes), then the streams join.  With
+        clip_norm the gradients' norm comes first (the flat buffer's padding
+        is zero)."""
+        if self.clip_norm is not None:
+            singa.grad_norm([self.g_flat], self.clip_norm, stat=self.grad_stat, workspace=self.norm_workspace)
         if self._issued is not None:
             self.wgrad_stream.wait_event(self._issued)
             with torch.cuda.stream(self.wgrad_stream):
@@ -474,14 +538,15 @@ class Net:
             self._update_ranges(self.update_ranges)
 
     def _update_ranges(self, ranges):
+        scale = None if self.clip_norm is None else self.grad_stat[1:]
         for a, e in ranges:
             wb = self.wb_flat[a:e] if self.wb_flat is not None else None
             if self.updater == "adagrad":
                 singa.adagrad_update(self.w_flat[a:e], self.g_flat[a:e], self.v_flat[a:e], wb, self.wl.lr,
-                                     self.adagrad_delta, self.wl.weight_decay)
+                                     self.adagrad_delta, self.wl.weight_decay, grad_scale=scale)
             else:
                 singa.sgd_momentum_update(self.w_flat[a:e], self.g_flat[a:e], self.v_flat[a:e], wb, self.wl.lr,
-                                          self.wl.momentum, self.wl.weight_decay)
+                                          self.wl.momentum, self.wl.weight_decay, grad_scale=scale)
 
     def train_one_batch(self, x, labels=None, dy_top=None, need_input_grad=False):
         self.forward(x, labels)

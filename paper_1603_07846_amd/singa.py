@@ -122,7 +122,7 @@ def _lib():
         lib.singa_trace_count.argtypes = []
         lib.singa_trace_get.argtypes = [i32, ctypes.POINTER(ctypes.c_char_p), ctypes.POINTER(ctypes.c_double),
                                         ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i32)]
-        pi, pp, ps = ctypes.POINTER(i32), ctypes.POINTER(vp), ctypes.POINTER(sz)
+        ps = ctypes.POINTER(sz)
         lib.singa_linear_fwd_workspace_bytes.argtypes = [i32, i32, i32, i32, ps]
         lib.singa_linear_fwd.argtypes = [i32, i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
         lib.singa_linear_bwd_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, ps]
@@ -131,8 +131,8 @@ def _lib():
         lib.singa_linear_softmax_ce.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, f32, vp, vp, vp, i32, vp, i32, vp,
                                                 sz, vp]
         lib.singa_grad_norm_workspace_bytes.argtypes = [i32]
-        lib.singa_grad_norm.argtypes = [i32, pi, pp, ps, f32, vp, vp, sz, vp]
-        lib.singa_grad_clip.argtypes = [i32, pi, pp, pp, ps, f32, vp, vp, sz, vp]
+        lib.singa_grad_norm.argtypes = [i32, vp, vp, vp, f32, vp, vp, sz, vp]
+        lib.singa_grad_clip.argtypes = [i32, vp, vp, vp, vp, f32, vp, vp, sz, vp]
         lib.singa_sgd_momentum_update_scaled.argtypes = [sz, vp, vp, vp, vp, f32, f32, f32, vp, vp]
         lib.singa_adagrad_update_scaled.argtypes = [sz, vp, vp, vp, vp, f32, f32, f32, vp, vp]
         for name in EXPORTS + DENSE_EXPORTS:
@@ -554,7 +554,8 @@ def _current() -> int:
 
 
 def _current_stream(cur):
-    return _raw_stream(cur) if _raw_stream is not None and torch.cuda.is_initialized() else _stream()
+    # (a tensor on the GPU is there: the runtime is initialized)
+    return _raw_stream(cur) if _raw_stream is not None else _stream()
 
 
 def _dense(name, t, dtype, shape, cur):
@@ -632,6 +633,11 @@ def _bytes(fn, *args) -> int:
     return out.value
 
 
+def grad_norm_workspace_bytes(count) -> int:
+    """Workspace of grad_norm and clip_grads over so many tensors."""
+    return _lib().singa_grad_norm_workspace_bytes(count)
+
+
 @functools.lru_cache(maxsize=1024)
 def linear_fwd_workspace_bytes(dtype, rows, din, dout) -> int:
     return _bytes("singa_linear_fwd_workspace_bytes", _dtype_code(dtype), rows, din, dout)
@@ -648,22 +654,47 @@ def linear_softmax_ce_workspace_bytes(dtype, rows, din, classes, grad=True, dw_d
                   _dtype_code(dw_dtype))
 
 
+class _LinearPlan:
+    """What follows from the shapes and the type of one linear_fwd alone.  Read-only once made."""
+
+    def __init__(self, x, w, act):
+        self.dt, _, self.din, self.dout = _rows(x, w)
+        self.act = _act(act)
+        self.rows = x.numel() // self.din
+        self.shape, self.cols = x.shape[:-1] + (self.dout,), torch.Size((self.dout,))
+        self.nbytes = linear_fwd_workspace_bytes(x.dtype, self.rows, self.din, self.dout)
+
+
+_LINEAR_PLANS = {}
+
+
 def linear_fwd(x, w, bias=None, act="none", residual=None, keep_z=False, out=None, z=None, workspace=None):
     """Inner product ComputeFeature: y = act(x w^T + bias) + residual, x (..., in), w (out, in), bias fp32.
     keep_z (or z, a tensor for it): also the pre-activation x w^T + bias, which linear_bwd takes; then (y, z) is
     returned.  act: "none", "relu", "gelu" (erf) or "silu"."""
-    dt, cur, din, dout = _rows(x, w)
-    a, dtype, device = _act(act), x.dtype, x.device
-    shape, rows = x.shape[:-1] + (dout,), x.numel() // din
+    dtype = x.dtype
+    key = (dtype, x.shape, w.shape, act)
+    p = _LINEAR_PLANS.get(key)
+    if p is None:
+        p = _LinearPlan(x, w, act)  # raises where the shapes or the type do not fit
+        if len(_LINEAR_PLANS) >= 1024:
+            _LINEAR_PLANS.clear()
+        _LINEAR_PLANS[key] = p
+    cur = _current() if x.is_cuda else -2
+    if not (w.dtype is dtype and x.is_contiguous() and w.is_contiguous() and x.get_device() == cur
+            and w.get_device() == cur):
+        _rows(x, w)  # says which
     if bias is not None:
-        _dense("bias", bias, torch.float32, (dout,), cur)
+        _dense("bias", bias, torch.float32, p.cols, cur)
     if residual is not None:
-        _dense("residual", residual, dtype, shape, cur)
-    y = _out("out", out, shape, dtype, device, cur)
+        _dense("residual", residual, dtype, p.shape, cur)
+    y = _ALLOC(p.shape, dtype, x.device) if out is None else _dense("out", out, dtype, p.shape, cur)
     if keep_z or z is not None:
-        z = _out("z", z, shape, dtype, device, cur)
-    ws, at, nbytes = _dense_ws(linear_fwd_workspace_bytes(dtype, rows, din, dout), device, workspace, cur)
-    rc = _LIB.singa_linear_fwd(dt, rows, din, dout, x.data_ptr(), w.data_ptr(), _ptr(bias), a, _ptr(residual), _ptr(z),
+        z = _out("z", z, p.shape, dtype, x.device, cur)
+    ws, at, nbytes = _dense_ws(p.nbytes, x.device, workspace, cur) if p.nbytes else (None, None, 0)
+    rc = _LIB.singa_linear_fwd(p.dt, p.rows, p.din, p.dout, x.data_ptr(), w.data_ptr(),
+                               None if bias is None else bias.data_ptr(), p.act,
+                               None if residual is None else residual.data_ptr(), None if z is None else z.data_ptr(),
                                y.data_ptr(), at, nbytes, _current_stream(cur))
     if rc:
         raise SingaError("singa_linear_fwd", rc)
@@ -741,10 +772,6 @@ def _grad_list(name, tensors, cur):
     return types, [t.numel() for t in tensors], [t.data_ptr() for t in tensors]
 
 
-def _c_array(kind, code, values):
-    return (kind * len(values)).from_buffer(array.array(code, values))
-
-
 def _grad_stat(grads, max_norm, out, stat, workspace):
     if not grads:
         raise ValueError("grads: at least one tensor wanted")
@@ -758,13 +785,14 @@ def _grad_stat(grads, max_norm, out, stat, workspace):
             raise ValueError("out: tensors of the gradients' sizes and types wanted")
     stat = _out("stat", stat, (2,), torch.float32, device, cur)
     ws, at, nbytes = _dense_ws(_LIB.singa_grad_norm_workspace_bytes(n), device, workspace, cur)
-    types, sizes = _c_array(ctypes.c_int, "i", types), _c_array(ctypes.c_size_t, "Q", sizes)
-    ptrs = _c_array(ctypes.c_void_p, "Q", ptrs)
+    # host arrays, read before the call returns
+    types, sizes, ptrs, outs = array.array("i", types), array.array("Q", sizes), array.array("Q", ptrs), array.array("Q", outs)
+    args = types.buffer_info()[0], ptrs.buffer_info()[0]
+    rest = sizes.buffer_info()[0], max_norm, stat.data_ptr(), at, nbytes, _current_stream(cur)
     if out is None:
-        rc = _LIB.singa_grad_norm(n, types, ptrs, sizes, max_norm, stat.data_ptr(), at, nbytes, _current_stream(cur))
+        rc = _LIB.singa_grad_norm(n, *args, *rest)
     else:
-        rc = _LIB.singa_grad_clip(n, types, ptrs, _c_array(ctypes.c_void_p, "Q", outs), sizes, max_norm, stat.data_ptr(),
-                                  at, nbytes, _current_stream(cur))
+        rc = _LIB.singa_grad_clip(n, *args, outs.buffer_info()[0], *rest)
     if rc:
         raise SingaError("singa_grad_norm" if out is None else "singa_grad_clip", rc)
     return stat
