@@ -82,8 +82,8 @@ def test_clipped_update_is_the_update_of_scaled_gradients(w, batch, updater):
 
 
 def test_captured_step_with_both():
-    net, x, labels = build(BF16, 24, fused_loss=True, clip_norm=0.5)
-    ref, _, _ = build(BF16, 24, fused_loss=True, clip_norm=0.5, concurrent_wgrad=False)
+    net, x, labels = build(BF16, 24, fused_loss=True, clip_norm=1e-2)
+    ref, _, _ = build(BF16, 24, fused_loss=True, clip_norm=1e-2, concurrent_wgrad=False)
     torch.cuda.synchronize()
     graph = net.capture(x, labels)
     for i in range(4):
