@@ -89,6 +89,11 @@ constexpr int K_TILE = 64;  // a multiple of every kernel's K-tile
 // Workspace for the partial sums of a product whose tiles cannot fill the GPU.
 size_t product_partial_bytes(int dt, int M, int N, int K, int epi);
 hipError_t launch_product(const Product& p, float* partial, hipStream_t st);
+// The products of a layer's source gradient (A K contiguous, B rows
+// contiguous) and weight gradient (both rows contiguous), in one launch where
+// that is faster; workspace: the larger of the two products' and this.
+size_t pair_partial_bytes(int dt, int Ma, int Na, int Ka, int Mb, int Nb, int Kb);
+hipError_t launch_pair(const Product& dx, const Product& dw, float* partial, hipStream_t st);
 // Number of partial sums of that product; launch_product with `raw` writes
 // them ([M][N rounded up to 8] each, also when it is one) and stops there.
 int product_splits(int dt, int M, int N, int K);

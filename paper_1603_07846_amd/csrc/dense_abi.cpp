@@ -93,6 +93,13 @@ size_t carve_fwd(int dt, int rows, int in, int out, void* ws, FwdWs* o) {
 }
 
 // ---------------------------------------------------------------- backward
+// Partial sums of the gradients' products, dx (rows x in over out) and dw (out
+// x in over kw), by themselves or together.
+size_t gradient_partial_bytes(int dt, int rows, int in, int out, int kw) {
+  return std::max({product_partial_bytes(dt, rows, in, out, EPI_OUT), product_partial_bytes(dt, out, in, kw, EPI_OUT),
+                   pair_partial_bytes(dt, rows, in, out, out, in, kw)});
+}
+
 struct BwdWs {
   Packed k;
   long ldz, rows_padded;
@@ -118,8 +125,8 @@ size_t carve_bwd(int dt, int rows, int in, int out, int act, int dw_dt, void* ws
   o->xp = c.take(o->k.copy ? (size_t)rows * o->k.ld * es : 0);
   o->wp = c.take(o->k.copy ? (size_t)out * o->k.ld * es : 0);
   o->colsum = c.take<float>(up(rows, COLSUM_ROWS) / COLSUM_ROWS * (size_t)out);
-  o->partial = (float*)c.take(std::max(product_partial_bytes(dt, rows, in, out, EPI_OUT),
-                                       product_partial_bytes(dt, out, in, (int)(o->rows_padded * (o->split ? TERMS : 1)), EPI_OUT)));
+  const int kw = (int)(o->rows_padded * (o->split ? TERMS : 1));
+  o->partial = (float*)c.take(gradient_partial_bytes(dt, rows, in, out, kw));
   return c.bytes();
 }
 
@@ -181,13 +188,18 @@ size_t carve_loss(int dt, int rows, int in, int classes, bool grad, int dw_dt, v
     // the last piece is shorter, and may be cut otherwise
     const int last = (int)(classes - (classes - 1) / o->piece * o->piece);
     for (int n : {(int)o->piece, last})
-      partial = std::max({partial, product_partial_bytes(dt, rows, in, n, EPI_OUT), product_partial_bytes(dt, n, in, kw, EPI_OUT)});
+      partial = std::max(partial, gradient_partial_bytes(dt, rows, in, n, kw));
   }
   o->partial = (float*)c.take(partial);
   return c.bytes();
 }
 
 Operand op(const void* p, long ld, bool kc) { return Operand{p, ld, kc}; }
+
+hipError_t launch_gradients(const Product* dx, const Product* dw, float* partial, hipStream_t st) {
+  if (dx && dw) return launch_pair(*dx, *dw, partial, st);
+  return dx || dw ? launch_product(dx ? *dx : *dw, partial, st) : hipSuccess;
+}
 
 }  // namespace
 
@@ -297,10 +309,10 @@ int singa_linear_bwd(singa_dtype dtype, int rows, int in, int out, const void* x
     x = o.xp;
     w = o.wp;
   }
-  Product p;
-  p.dt = dtype;
-  p.flops = 2.0 * rows * in * out;
-  if (dx && e == hipSuccess) {
+  Product p, q;
+  p.dt = q.dt = dtype;
+  p.flops = q.flops = 2.0 * rows * in * out;
+  if (dx) {
     p.name = "product_kernel<bwd_data>";
     p.M = rows;
     p.N = in;
@@ -309,23 +321,21 @@ int singa_linear_bwd(singa_dtype dtype, int rows, int in, int out, const void* x
     p.b = op(w, o.k.ld, false);
     p.e.res = dx_residual;
     p.e.y = dx;
-    e = launch_product(p, o.partial, st);
   }
-  if (dw && e == hipSuccess) {
-    p.name = "product_kernel<bwd_weights>";
-    p.M = out;
-    p.N = in;
-    p.K = split ? (int)(TERMS * o.rows_padded) : rows;
-    p.wrap = split ? (int)o.rows_padded : 0;
-    p.kb = rows;
-    p.a = op(dz, o.ldz, false);
-    p.b = op(x, o.k.ld, false);
-    p.e = Epilogue{};
-    p.e.y = dw;
-    p.e.out_f32 = dw_dtype == SINGA_F32;
-    p.e.add = accumulate != 0;
-    e = launch_product(p, o.partial, st);
+  if (dw) {
+    q.name = "product_kernel<bwd_weights>";
+    q.M = out;
+    q.N = in;
+    q.K = split ? (int)(TERMS * o.rows_padded) : rows;
+    q.wrap = split ? (int)o.rows_padded : 0;
+    q.kb = rows;
+    q.a = op(dz, o.ldz, false);
+    q.b = op(x, o.k.ld, false);
+    q.e.y = dw;
+    q.e.out_f32 = dw_dtype == SINGA_F32;
+    q.e.add = accumulate != 0;
   }
+  if (e == hipSuccess) e = launch_gradients(dx ? &p : nullptr, dw ? &q : nullptr, o.partial, st);
   return status(e);
 }
 
@@ -474,8 +484,8 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
       e = launch_colsum_rows(o.logits, o.ldl, o.colsum, rows, classes, labels, classes, st);
     }
     if (e == hipSuccess && db && !finish) e = launch_colsum(o.colsum, db + c0, groups, n, accumulate, o.unit, st);
-    if (e == hipSuccess && dx) {
-      Product q;
+    Product q, v;
+    if (dx) {
       q.name = "product_kernel<bwd_data>";
       q.dt = dtype;
       q.flops = 2.0 * rows * in * n;
@@ -492,26 +502,24 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
         q.e.labels = labels;
         q.e.classes = classes;
       }
-      e = launch_product(q, o.partial, st);
     }
-    if (e == hipSuccess && dw) {
-      Product q;
-      q.name = "product_kernel<bwd_weights>";
-      q.dt = dtype;
-      q.flops = 2.0 * rows * in * n;
-      q.M = n;
-      q.N = in;
-      q.K = split ? (int)(TERMS * o.rows_padded) : rows;
-      q.wrap = split ? (int)o.rows_padded : 0;
-      q.kb = rows;
-      q.a = op(o.dz, o.ldd, false);
-      q.b = op(o.xc, o.k.ld, false);
-      q.e.alpha = o.unit;
-      q.e.y = (char*)dw + c0 * in * (long)dt_size(dw_dtype);
-      q.e.out_f32 = dw_dtype == SINGA_F32;
-      q.e.add = accumulate != 0;
-      e = launch_product(q, o.partial, st);
+    if (dw) {
+      v.name = "product_kernel<bwd_weights>";
+      v.dt = dtype;
+      v.flops = 2.0 * rows * in * n;
+      v.M = n;
+      v.N = in;
+      v.K = split ? (int)(TERMS * o.rows_padded) : rows;
+      v.wrap = split ? (int)o.rows_padded : 0;
+      v.kb = rows;
+      v.a = op(o.dz, o.ldd, false);
+      v.b = op(o.xc, o.k.ld, false);
+      v.e.alpha = o.unit;
+      v.e.y = (char*)dw + c0 * in * (long)dt_size(dw_dtype);
+      v.e.out_f32 = dw_dtype == SINGA_F32;
+      v.e.add = accumulate != 0;
     }
+    if (e == hipSuccess) e = launch_gradients(dx ? &q : nullptr, dw ? &v : nullptr, o.partial, st);
   }
   if (e == hipSuccess && dx && !o.one) e = launch_round_rows(dtype, o.dxf, dx, rows, in, labels, classes, st);
   return status(e);

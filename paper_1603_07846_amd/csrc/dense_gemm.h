@@ -398,7 +398,7 @@ template <typename T, bool KC, int R, int F> struct Frags {
   }
 };
 
-// WM x WN waves of (32 FM) x (32 FN).
+// A tile: WM x WN waves of (32 FM) x (32 FN).
 //
 // A K-tile is four steps of FM x FN matrix instructions (per 16 bytes of k).
 // Between the instructions of a step the wave reads the fragments of the next
@@ -408,23 +408,30 @@ template <typename T, bool KC, int R, int F> struct Frags {
 // that the barrier has freed; the other loads follow in the next step (64 KB in
 // one step of 512 cycles were twice what the vector memory path takes: 870 ->
 // 833 us at 8192^3).  A barrier waits for loads issued at least two steps ago.
-template <typename T, bool AKC, bool BKC, int WM, int WN, int FM, int FN, int EPI>
-__global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(GemmArgs g) {
-  constexpr int NW = WM * WN, BM = WM * FM * 32, BN = WN * FN * 32;
+template <typename T, bool AKC, bool BKC, int WM, int WN, int FM, int FN> struct Shape {
+  static constexpr int NW = WM * WN, BM = WM * FM * 32, BN = WN * FN * 32;
   typedef Tile<T, AKC, BM, NW> TA;
   typedef Tile<T, BKC, BN, NW> TB;
-  constexpr int STAGE = TA::BYTES + TB::BYTES;
-  constexpr int PIT = FN == 4 ? 152 : 88, HALF = FN * 16 + 16;  // floats per staged row; where its odd groups start
-  static_assert((FN == 2 || FN == 4) && PIT % 16 == 8 && PIT >= HALF + FN * 16, "rows 4 apart lie half the banks apart");
-  constexpr int SMEM = 2 * STAGE > NW * 32 * PIT * 4 + BM * 8 ? 2 * STAGE : NW * 32 * PIT * 4 + BM * 8;
-  __shared__ __align__(1024) char smem[SMEM];
+  static constexpr int STAGE = TA::BYTES + TB::BYTES;
+  static constexpr int PIT = FN == 4 ? 152 : FN == 2 ? 88 : 56, HALF = FN * 16 + 16;  // floats per staged row; where its odd groups start
+  static_assert(PIT % 16 == 8 && PIT >= HALF + FN * 16, "rows 4 apart lie half the banks apart");
+  static constexpr int SMEM = 2 * STAGE > NW * 32 * PIT * 4 + BM * 8 ? 2 * STAGE : NW * 32 * PIT * 4 + BM * 8;
+};
+
+// Workgroup `wg` of a product's tiles x splits.
+template <typename T, bool AKC, bool BKC, int WM, int WN, int FM, int FN, int EPI>
+__device__ __forceinline__ void product_tile(const GemmArgs& g, int wg, char* smem) {
+  typedef Shape<T, AKC, BKC, WM, WN, FM, FN> S;
+  typedef typename S::TA TA;
+  typedef typename S::TB TB;
+  constexpr int NW = S::NW, BM = S::BM, BN = S::BN, STAGE = S::STAGE, PIT = S::PIT, HALF = S::HALF;
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   // tiles in groups of 8 tile rows, column by column, dealt to the XCDs in
   // contiguous runs: neighbours share operand rows in one L2
   const int tiles = g.tiles_m * g.tiles_n;
-  const int split = blockIdx.x / tiles;
-  int t = xcd_remap(blockIdx.x - split * tiles, tiles);
+  const int split = wg / tiles;
+  int t = xcd_remap(wg - split * tiles, tiles);
   constexpr int GM = 8;
   const int group = t / (GM * g.tiles_n), first = group * GM, gm = min(GM, g.tiles_m - first);
   t -= group * GM * g.tiles_n;
@@ -528,7 +535,8 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(G
           af[nxt][f - FN] = fa.read(s, f - FN, ks);
       }
       if constexpr (PREPARE) {
-        if (n % (N / 4) == 0) prepare(n / (N / 4));
+#pragma unroll
+        for (int part = n * 4 / N; part < (n + 1) * 4 / N; ++part) prepare(part);
       }
 #pragma unroll
       for (int l = L0 + n * (L1 - L0) / N; l < L0 + (n + 1) * (L1 - L0) / N; ++l) load(l, stage);
@@ -675,7 +683,9 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(G
   for (int bm = 0; bm < FM; ++bm) {
     const int row0 = m0 + (wm * FM + bm) * 32;
     if (bm == 0) stage_block(Const<0>{});
-    if (bm == 1) stage_block(Const<1>{});
+    if constexpr (FM >= 2) {
+      if (bm == 1) stage_block(Const<1>{});
+    }
     if constexpr (FM == 4) {
       if (bm == 2) stage_block(Const<2>{});
       if (bm == 3) stage_block(Const<3>{});
@@ -746,7 +756,7 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(G
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += cols.bias[j];
         if constexpr (EPI == EPI_LSE) {
-          static_assert(FN * 32 % STAT_COLS == 0, "whole groups of columns");
+          static_assert(EPI != EPI_LSE || FN * 32 % STAT_COLS == 0, "whole groups of columns");
           constexpr int LPG = STAT_COLS / 8;  // lanes per group
           if (edge) {
 #pragma unroll
@@ -804,6 +814,7 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(G
     }
     __builtin_amdgcn_wave_barrier();
     if constexpr (EPI == EPI_DLOGITS) {
+      static_assert(FM * 32 % COLSUM_ROWS == 0 || EPI != EPI_DLOGITS, "whole groups of rows");
       if (((bm + 1) * 32) % COLSUM_ROWS == 0) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -822,6 +833,28 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : 2) void product_kernel(G
       }
     }
   }
+}
+
+template <typename T, bool AKC, bool BKC, int WM, int WN, int FM, int FN, int EPI>
+__global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : FM == 2 ? 2 : 4) void product_kernel(GemmArgs g) {
+  __shared__ __align__(1024) char smem[Shape<T, AKC, BKC, WM, WN, FM, FN>::SMEM];
+  product_tile<T, AKC, BKC, WM, WN, FM, FN, EPI>(g, blockIdx.x, smem);
+}
+
+// The two products of a layer's gradients in one launch, source gradient
+// first: neither leaves the chip half empty while the other waits.
+struct PairArgs {
+  GemmArgs dx, dw;
+  int wgs_dx;
+};
+template <typename T, int FM, int FN>
+__global__ __launch_bounds__(256, FM == 4 ? 1 : FM == 2 ? 2 : 4) void product_pair_kernel(PairArgs p) {
+  constexpr int S1 = Shape<T, true, false, 2, 2, FM, FN>::SMEM, S2 = Shape<T, false, false, 2, 2, FM, FN>::SMEM;
+  __shared__ __align__(1024) char smem[S1 > S2 ? S1 : S2];
+  if ((int)blockIdx.x < p.wgs_dx)
+    product_tile<T, true, false, 2, 2, FM, FN, EPI_OUT>(p.dx, blockIdx.x, smem);
+  else
+    product_tile<T, false, false, 2, 2, FM, FN, EPI_OUT>(p.dw, (int)blockIdx.x - p.wgs_dx, smem);
 }
 
 // Adds the partial sums of a split product in order and finishes them.
@@ -863,60 +896,97 @@ template <typename T> __global__ __launch_bounds__(256) void product_reduce_kern
       [] {});
 }
 
+// ------------------------------------------------------------------ plans
+//
+// Tiles of 256 x 256 (bf16), 128 x 128, or 64 x 64 (fp32, whose matrix
+// instructions are slow enough for the smaller tile's loads), and the cut of
+// the K range, from a model of the time in us that follows what was measured
+// (MI355X, 24 products of 128 .. 4096 rows, 256 .. 32768 of k).  A K-tile takes
+//   256: 1.42, and 10 per tile; one workgroup per CU
+//   128: bf16 0.44 while there is one workgroup per CU and 1.0 at two, fp32
+//        1.95 times the workgroups per CU; 5 per tile
+//   64:  0.55 times the workgroups per CU; 4 per tile
+// and a cut costs the second launch, 4, and its partial sums' bytes at 6 TB/s.
+enum { TILE_128 = 0, TILE_256 = 1, TILE_64 = 2 };
 struct Plan {
-  int big, splits, kt_split;
+  int tile, splits, kt_split;
+  double t;
 };
+inline long div_up(long a, long b) { return (a + b - 1) / b; }
+inline int tile_rows(int tile) { return tile == TILE_256 ? 256 : tile == TILE_64 ? 64 : 128; }
+inline long tiles_of(int tile, int M, int N) { return div_up(M, tile_rows(tile)) * div_up(N, tile_rows(tile)); }
+inline bool tile_ok(int tile, int dt, int epi) { return tile == TILE_128 || (tile == TILE_256 ? dt == BF16 : dt == F32 && epi == EPI_OUT); }
+inline int ktiles(int dt, int K) { return (int)div_up(K, dt == BF16 ? 64 : 32); }
 
-// The tile and the cut of the K range, from a model of the time in us that
-// follows what was measured (MI355X, 24 products of 128 .. 4096 rows, 256 ..
-// 32768 of k): a K-tile takes 1.42 in a 256 x 256 tile (bf16, one workgroup
-// per CU, 10 more per tile); in a 128 x 128 tile 0.44 (fp32 1.95) while there
-// is one workgroup per CU and 1.0 (3.9) at two, 5 more per tile; a cut costs
-// the second launch, 4, and its partial sums' bytes at some 6 TB/s.
+// Workgroups that run at once, and the time of one of `per` K-tiles while `n`
+// are there.
+inline int slots_of(int tile, int dt) { return tile == TILE_128 && dt == BF16 ? 512 : 256; }
+inline double wg_time(int tile, int dt, long per, long n) {
+  if (tile == TILE_256) return per * 1.42 + 10;
+  if (tile == TILE_64) return per * 0.55 + 4;
+  if (dt == F32) return per * 1.95 + 5;
+  return per * (n <= 256 ? 0.44 : n >= 512 ? 1.0 : 0.44 + (n - 256) / 256.0 * 0.56) + 5;
+}
+inline double cut_time(int s, int M, int N) { return s > 1 ? 4 + s * (double)M * N * 8 / 6e6 : 0; }
+
 inline Plan plan_product(int dt, int M, int N, int K, int epi) {
-  auto up = [](long a, long b) { return (a + b - 1) / b; };
-  const int kt = (int)up(K, dt == BF16 ? 64 : 32);
-  Plan p{0, 1, kt};
-  double best = 1e30;
-  for (int big = 0; big < (dt == BF16 ? 2 : 1); ++big) {
-    const long tiles = big ? up(M, 256) * up(N, 256) : up(M, 128) * up(N, 128);
+  const int kt = ktiles(dt, K);
+  Plan best{TILE_128, 1, kt, 1e30};
+  for (int tile = 0; tile < 3; ++tile) {
+    if (!tile_ok(tile, dt, epi)) continue;
+    const long tiles = tiles_of(tile, M, N);
     for (int s = 1; s <= 32 && s <= kt && (s == 1 || epi == EPI_OUT); ++s) {
-      const long n = tiles * s;
-      if (s > 1 && n > 512) break;
-      const long per = up(kt, s);
-      double t;
-      if (big)
-        t = (double)up(n, 256) * (per * 1.42 + 10);
-      else if (dt == BF16)
-        t = (double)up(n, 512) * (per * (n <= 256 ? 0.44 : n >= 512 ? 1.0 : 0.44 + (n - 256) / 256.0 * 0.56) + 5);
-      else
-        t = (double)up(n, 256) * per * 1.95 + (double)up(n, 512) * 5;
-      if (s > 1) t += 4 + s * (double)M * N * 8 / 6e6;
-      if (t < best) {
-        best = t;
-        p.big = big;
-        p.kt_split = (int)per;
-        p.splits = (int)up(kt, per);
-      }
+      const long n = tiles * s, per = div_up(kt, s);
+      if (s > 1 && n > 1024) break;
+      const double t = div_up(n, slots_of(tile, dt)) * wg_time(tile, dt, per, n) + cut_time(s, M, N);
+      if (t < best.t) best = Plan{tile, (int)div_up(kt, per), (int)per, t};
     }
   }
-  return p;
+  return best;
 }
 
-template <typename T, bool AKC, bool BKC, int EPI> hipError_t launch_tiles(const Product& p, const GemmArgs& g, bool big, hipStream_t st) {
-  const dim3 grid((unsigned)((long)g.tiles_m * g.tiles_n * g.splits));
-  TraceScope ts(p.name, st, p.flops, WORK_FLOP);
-  if (sizeof(T) == 2 && big)
-    hipLaunchKernelGGL((product_kernel<T, AKC, BKC, 2, 2, sizeof(T) == 2 ? 4 : 2, sizeof(T) == 2 ? 4 : 2, EPI>), grid, dim3(256), 0, st, g);
-  else
-    hipLaunchKernelGGL((product_kernel<T, AKC, BKC, 2, 2, 2, 2, EPI>), grid, dim3(256), 0, st, g);
-  return hipGetLastError();
+// The same for two products in one launch (of one tile): as long as the longer
+// workgroup, or as all of them over the slots and half of a shorter one at the
+// end.
+struct PairPlan {
+  Plan a, b;
+  double t;
+};
+inline PairPlan plan_pair(int dt, int Ma, int Na, int Ka, int Mb, int Nb, int Kb) {
+  static const int cuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
+  const int ka = ktiles(dt, Ka), kb = ktiles(dt, Kb);
+  PairPlan best{{}, {}, 1e30};
+  for (int tile = 0; tile < 3; ++tile) {
+    if (!tile_ok(tile, dt, EPI_OUT)) continue;
+    const long ta = tiles_of(tile, Ma, Na), tb = tiles_of(tile, Mb, Nb);
+    const int slots = slots_of(tile, dt);
+    for (int sa : cuts)
+      for (int sb : cuts) {
+        if (sa > ka || sb > kb) continue;
+        const long na = ta * sa, nb = tb * sb, pa = div_up(ka, sa), pb = div_up(kb, sb);
+        if ((sa > 1 && na > 1024) || (sb > 1 && nb > 1024)) continue;
+        const double da = wg_time(tile, dt, pa, na + nb), db = wg_time(tile, dt, pb, na + nb);
+        double t = da > db ? da : db;
+        const double all = (na * da + nb * db) / slots + (na + nb > slots ? 0.5 * (da < db ? da : db) : 0);
+        if (all > t) t = all;
+        t += cut_time(sa, Ma, Na) + cut_time(sb, Mb, Nb);
+        if (t < best.t) best = PairPlan{{tile, (int)div_up(ka, pa), (int)pa, t}, {tile, (int)div_up(kb, pb), (int)pb, t}, t};
+      }
+  }
+  return best;
+}
+// One launch, unless the two products by themselves are faster (a launch: 3).
+inline bool pair_pays(int dt, const PairPlan& p, int Ma, int Na, int Ka, int Mb, int Nb, int Kb) {
+  return p.t < plan_product(dt, Ma, Na, Ka, EPI_OUT).t + plan_product(dt, Mb, Nb, Kb, EPI_OUT).t + 3;
+}
+inline size_t partial_bytes_of(const Plan& p, int M, int N) {
+  return p.splits > 1 ? (size_t)p.splits * M * (((size_t)N + 7) / 8 * 8) * 4 : 0;
 }
 
-template <typename T> hipError_t launch_product_t(const Product& p, float* partial, hipStream_t st) {
+// --------------------------------------------------------------- launches
+template <typename T> GemmArgs args_of(const Product& p, const Plan& pl, float* partial) {
   constexpr int ES = (int)sizeof(T), VEC = TypeInfo<T>::VEC;
-  const Plan pl = plan_product(p.dt, p.M, p.N, p.K, p.epi);
-  const int bm = pl.big ? 256 : 128;
+  const int bm = tile_rows(pl.tile);
   GemmArgs g{};
   const long kb = p.kb ? p.kb : p.K;
   g.a = (const char*)p.a.p;
@@ -928,7 +998,7 @@ template <typename T> hipError_t launch_product_t(const Product& p, float* parti
   g.M = p.M;
   g.N = p.N;
   g.kca = g.kcb = (p.K + VEC - 1) / VEC;
-  g.kt_all = (p.K + TypeInfo<T>::BK - 1) / TypeInfo<T>::BK;
+  g.kt_all = ktiles(p.dt, p.K);
   g.kt_split = pl.kt_split;
   g.splits = pl.splits;
   g.wrap = p.wrap / TypeInfo<T>::BK;
@@ -940,19 +1010,72 @@ template <typename T> hipError_t launch_product_t(const Product& p, float* parti
   g.vec = p.N % 8 == 0;
   g.e = p.e;
   if (!g.e.ldy) g.e.ldy = p.N;
-  hipError_t e = hipErrorNotSupported;
-  if (p.epi == EPI_OUT) {
-    if (p.a.kc && p.b.kc) e = launch_tiles<T, true, true, EPI_OUT>(p, g, pl.big, st);
-    if (p.a.kc && !p.b.kc) e = launch_tiles<T, true, false, EPI_OUT>(p, g, pl.big, st);
-    if (!p.a.kc && !p.b.kc) e = launch_tiles<T, false, false, EPI_OUT>(p, g, pl.big, st);
-  } else if (p.a.kc && p.b.kc) {
-    e = p.epi == EPI_LSE ? launch_tiles<T, true, true, EPI_LSE>(p, g, pl.big, st)
-                         : launch_tiles<T, true, true, EPI_DLOGITS>(p, g, pl.big, st);
-  }
-  if (e != hipSuccess || g.splits == 1 || p.raw) return e;
+  return g;
+}
+
+template <typename T> hipError_t launch_reduce(const Product& p, const GemmArgs& g, hipStream_t st) {
+  if (g.splits == 1 || p.raw) return hipSuccess;
   TraceScope ts("product_reduce_kernel", st, 4.0 * (g.splits + 1) * p.M * p.N, WORK_BYTE);
   hipLaunchKernelGGL(product_reduce_kernel<T>, dim3((unsigned)(((long)p.M * (g.ldp / 8) + 255) / 256)), dim3(256), 0, st, g);
   return hipGetLastError();
+}
+
+inline long wgs_of(const GemmArgs& g) { return (long)g.tiles_m * g.tiles_n * g.splits; }
+
+template <typename T, bool AKC, bool BKC, int EPI> hipError_t launch_tiles(const Product& p, const GemmArgs& g, int tile, hipStream_t st) {
+  const dim3 grid((unsigned)wgs_of(g));
+  TraceScope ts(p.name, st, p.flops, WORK_FLOP);
+  constexpr bool F = sizeof(T) == 4;
+  if (!F && tile == TILE_256)
+    hipLaunchKernelGGL((product_kernel<T, AKC, BKC, 2, 2, F ? 2 : 4, F ? 2 : 4, EPI>), grid, dim3(256), 0, st, g);
+  else if (F && EPI == EPI_OUT && tile == TILE_64)
+    hipLaunchKernelGGL((product_kernel<T, AKC, BKC, 2, 2, F && EPI == EPI_OUT ? 1 : 2, F && EPI == EPI_OUT ? 1 : 2, EPI>), grid,
+                       dim3(256), 0, st, g);
+  else
+    hipLaunchKernelGGL((product_kernel<T, AKC, BKC, 2, 2, 2, 2, EPI>), grid, dim3(256), 0, st, g);
+  return hipGetLastError();
+}
+
+template <typename T> hipError_t launch_product_t(const Product& p, float* partial, hipStream_t st) {
+  const Plan pl = plan_product(p.dt, p.M, p.N, p.K, p.epi);
+  const GemmArgs g = args_of<T>(p, pl, partial);
+  hipError_t e = hipErrorNotSupported;
+  if (p.epi == EPI_OUT) {
+    if (p.a.kc && p.b.kc) e = launch_tiles<T, true, true, EPI_OUT>(p, g, pl.tile, st);
+    if (p.a.kc && !p.b.kc) e = launch_tiles<T, true, false, EPI_OUT>(p, g, pl.tile, st);
+    if (!p.a.kc && !p.b.kc) e = launch_tiles<T, false, false, EPI_OUT>(p, g, pl.tile, st);
+  } else if (p.a.kc && p.b.kc) {
+    e = p.epi == EPI_LSE ? launch_tiles<T, true, true, EPI_LSE>(p, g, pl.tile, st)
+                         : launch_tiles<T, true, true, EPI_DLOGITS>(p, g, pl.tile, st);
+  }
+  return e == hipSuccess ? launch_reduce<T>(p, g, st) : e;
+}
+
+template <typename T> hipError_t launch_pair_t(const Product& dx, const Product& dw, float* partial, hipStream_t st) {
+  const PairPlan pl = plan_pair(dx.dt, dx.M, dx.N, dx.K, dw.M, dw.N, dw.K);
+  if (!pair_pays(dx.dt, pl, dx.M, dx.N, dx.K, dw.M, dw.N, dw.K)) {
+    const hipError_t e = launch_product_t<T>(dx, partial, st);
+    return e == hipSuccess ? launch_product_t<T>(dw, partial, st) : e;
+  }
+  PairArgs a;
+  a.dx = args_of<T>(dx, pl.a, partial);
+  a.dw = args_of<T>(dw, pl.b, partial + partial_bytes_of(pl.a, dx.M, dx.N) / 4);
+  a.wgs_dx = (int)wgs_of(a.dx);
+  const dim3 grid((unsigned)(wgs_of(a.dx) + wgs_of(a.dw)));
+  {
+    TraceScope ts("product_pair_kernel", st, dx.flops + dw.flops, WORK_FLOP);
+    constexpr bool F = sizeof(T) == 4;
+    if (!F && pl.a.tile == TILE_256)
+      hipLaunchKernelGGL((product_pair_kernel<T, F ? 2 : 4, F ? 2 : 4>), grid, dim3(256), 0, st, a);
+    else if (F && pl.a.tile == TILE_64)
+      hipLaunchKernelGGL((product_pair_kernel<T, F ? 1 : 2, F ? 1 : 2>), grid, dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL((product_pair_kernel<T, 2, 2>), grid, dim3(256), 0, st, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const hipError_t e = launch_reduce<T>(dx, a.dx, st);
+  return e == hipSuccess ? launch_reduce<T>(dw, a.dw, st) : e;
 }
 
 }  // namespace
