@@ -14,7 +14,7 @@
  *     singa_grad_norm / _clip at their element size.
  *   - the matrices' sizes are free (1 and odd ones included); a row whose
  *     length is no multiple of 16 bytes costs a copy of its matrix in the
- *     workspace, except in the pass over the weights that up to 64 rows take.
+ *     workspace, except in the pass over the weights that few rows take.
  *   - the workspace has no alignment but 16 bytes and needs no clearing; two
  *     calls whose execution may overlap need one each.
  *   - outputs may not overlap inputs unless stated.

@@ -98,6 +98,8 @@ hipError_t launch_pair(const Product& dx, const Product& dw, float* partial, hip
 // them ([M][N rounded up to 8] each, also when it is one) and stops there.
 int product_splits(int dt, int M, int N, int K);
 
+// Whether launch_skinny is the faster one.
+bool product_skinny(int dt, int M, int N, int K);
 // The same product for few rows (M <= SKINNY_ROWS), A and B both K contiguous
 // with ld = K, any alignment: a pass over B.  EPI_OUT and EPI_LSE (STAT_COLS
 // of SKINNY_COLS columns).
@@ -156,7 +158,10 @@ struct LossRows {
   void* xc;
   int in;
   long ldx;
+  float2* stats;  // [rows][loss_parts(classes)]: several workgroups per row; null: one
 };
+constexpr int LOSS_PART = 4096;  // classes per workgroup then
+inline int loss_parts(int classes) { return (classes + LOSS_PART - 1) / LOSS_PART; }
 hipError_t launch_loss_rows(int dt, const LossRows& a, hipStream_t st);
 // The mean and the unit (may be null) of up to FINISH_ROWS rows and, unless db
 // is null, db (+)= unit times the sum of the valid rows of dz.

@@ -73,6 +73,7 @@ Packed packed(int dt, int cols) {
 
 // ---------------------------------------------------------------- forward
 struct FwdWs {
+  bool skinny;
   Packed k;
   void *xp, *wp;
   float* partial;
@@ -80,10 +81,9 @@ struct FwdWs {
 
 size_t carve_fwd(int dt, int rows, int in, int out, void* ws, FwdWs* o) {
   Carver c(ws);
-  if (rows == 0 || rows <= SKINNY_ROWS) {
-    *o = FwdWs{};
-    return 0;
-  }
+  *o = FwdWs{};
+  o->skinny = product_skinny(dt, rows, out, in);
+  if (rows == 0 || o->skinny) return 0;
   const size_t es = dt_size(dt);
   o->k = packed(dt, in);
   o->xp = c.take(o->k.copy ? (size_t)rows * o->k.ld * es : 0);
@@ -151,7 +151,8 @@ size_t carve_loss(int dt, int rows, int in, int classes, bool grad, int dw_dt, v
   if (rows == 0) return 0;
   const size_t es = dt_size(dt);
   o->k = packed(dt, in);
-  o->skinny = rows <= SKINNY_ROWS;
+  // (the loss of a few rows alone takes two launches that way, four after tiles)
+  o->skinny = product_skinny(dt, rows, classes, in) || (!grad && rows <= LSE_FINISH_ROWS);
   o->ldl = up(classes, 8);
   o->keep = (!o->skinny || grad) && (size_t)rows * o->ldl * 4 <= kKeep;
   o->split = grad && dt == BF16 && dw_dt == F32;
@@ -164,6 +165,8 @@ size_t carve_loss(int dt, int rows, int in, int classes, bool grad, int dw_dt, v
   if (o->keep) {
     o->splits = o->skinny ? 1 : product_splits(dt, rows, classes, in);
     o->logits = c.take<float>((size_t)o->splits * rows * o->ldl);
+    // rows that do not fill the chip, and several parts of each
+    o->stats = rows < 512 && classes > 2 * LOSS_PART ? c.take<float2>((size_t)rows * loss_parts(classes)) : nullptr;
   } else {
     o->nstat = (classes + (o->skinny ? SKINNY_COLS : STAT_COLS) - 1) / (o->skinny ? SKINNY_COLS : STAT_COLS);
     o->stats = c.take<float2>((size_t)rows * o->nstat);
@@ -242,7 +245,7 @@ int singa_linear_fwd(singa_dtype dtype, int rows, int in, int out, const void* x
   p.e.res = residual;
   p.e.z = z;
   p.e.y = y;
-  if (rows <= SKINNY_ROWS) {
+  if (o.skinny) {
     p.name = "skinny_kernel";
     p.a = op(x, in, true);
     p.b = op(w, in, true);
@@ -423,6 +426,7 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
     r.rows_padded = o.rows_padded;
     r.classes = classes;
     r.loss = loss;
+    r.stats = o.stats;
     if (!grad) {
       r.rows_padded = rows;
     } else {

@@ -12,8 +12,9 @@ namespace {
 // Reads B (the weights) once, 16 of its rows per workgroup, straight into
 // registers: v_mfma_f32_16x16x32_bf16 (or four v_mfma_f32_16x16x4_f32) takes
 // 16 bytes of a row from each lane, 64 consecutive bytes of a row per step, so
-// neither operand needs LDS and any row start will do (ALIGNED: 16-byte
-// loads; otherwise element loads).  The waves share the K range and add their
+// neither operand needs LDS and any row start will do (ALIGNED: the rows start
+// at 16-byte boundaries; otherwise the same loads without that promise, and the
+// end of a row element by element).  The waves share the K range and add their
 // sums through LDS.  Bound by the bytes of B; U steps (U x 64 bytes of 16
 // rows) are in flight per wave.
 typedef float f32x4v __attribute__((ext_vector_type(4)));
@@ -26,18 +27,23 @@ __device__ __forceinline__ void mma16(const f32x4& a, const f32x4& b, f32x4v& c)
   for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
 }
 
-// 16 bytes of a row from element k (k < K; elements from K on are zero)
-template <typename T, bool ALIGNED>
-__device__ __forceinline__ typename Chunk<T>::type row_chunk(const T* row, int k, int K) {
+// 16 bytes of a row from element k, all of them within it
+template <typename T, bool ALIGNED> __device__ __forceinline__ typename Chunk<T>::type row_chunk(const T* row, int k) {
+  typename Chunk<T>::type c;
+  if constexpr (ALIGNED)
+    c = *(const typename Chunk<T>::type*)(row + k);
+  else
+    __builtin_memcpy(&c, row + k, 16);
+  return c;
+}
+// the same near the row's end: elements from K on are zero
+template <typename T, bool ALIGNED> __device__ __forceinline__ typename Chunk<T>::type row_end(const T* row, int k, int K) {
   constexpr int VEC = TypeInfo<T>::VEC;
-  if constexpr (ALIGNED) {
-    return *(const typename Chunk<T>::type*)(row + k);
-  } else {
-    union { typename Chunk<T>::type c; T e[VEC]; } u;
+  if (k + VEC <= K) return row_chunk<T, ALIGNED>(row, k);
+  union { typename Chunk<T>::type c; T e[VEC]; } u;
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) u.e[j] = k + j < K ? row[k + j] : zero_elem<T>();
-    return u.c;
-  }
+  for (int j = 0; j < VEC; ++j) u.e[j] = k + j < K ? row[k + j] : zero_elem<T>();
+  return u.c;
 }
 
 constexpr int SKINNY_WAVES = 4;
@@ -63,11 +69,11 @@ __global__ __launch_bounds__(SKINNY_WAVES * 64) void skinny_kernel(const T* __re
     const int k = it * STEP * U + kq * VEC;
     C wc[U], xc[MT][U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) wc[u] = row_chunk<T, ALIGNED>(wr, k + u * STEP, K);
+    for (int u = 0; u < U; ++u) wc[u] = row_chunk<T, ALIGNED>(wr, k + u * STEP);
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int u = 0; u < U; ++u) xc[m][u] = row_chunk<T, ALIGNED>(xr[m], k + u * STEP, K);
+      for (int u = 0; u < U; ++u) xc[m][u] = row_chunk<T, ALIGNED>(xr[m], k + u * STEP);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -78,9 +84,9 @@ __global__ __launch_bounds__(SKINNY_WAVES * 64) void skinny_kernel(const T* __re
     const int k = k0 + kq * VEC;
     C wc{}, xc[MT]{};
     if (k < K) {
-      wc = row_chunk<T, ALIGNED>(wr, k, K);
+      wc = row_end<T, ALIGNED>(wr, k, K);
 #pragma unroll
-      for (int m = 0; m < MT; ++m) xc[m] = row_chunk<T, ALIGNED>(xr[m], k, K);
+      for (int m = 0; m < MT; ++m) xc[m] = row_end<T, ALIGNED>(xr[m], k, K);
     }
 #pragma unroll
     for (int m = 0; m < MT; ++m) mma16(wc, xc[m], acc[m]);
@@ -449,6 +455,96 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(LossRows a) {
   }
 }
 
+// The same for many classes, LOSS_PART of them per workgroup (x: of the row,
+// y: part), in two launches: the first adds the partial sums up, leaves the
+// logits and the part's maximum and sum, and cleans x; the second merges the
+// parts' and does the rest.
+__global__ __launch_bounds__(256) void loss_parts_kernel(LossRows a, float2* __restrict__ stats, int parts) {
+  __shared__ float2 lds[4];
+  const long row = blockIdx.x;
+  if (!label_ok(a.labels[row], a.classes)) return;
+  constexpr int U = 4;
+  float* zr = a.z + (size_t)row * a.ldz;
+  const size_t step = (size_t)a.rows * a.ldz;
+  const int end = min(a.classes, (int)(blockIdx.y + 1) * LOSS_PART);
+  float m = -INFINITY, s = 0.f;
+  for (int c0 = blockIdx.y * LOSS_PART + threadIdx.x; c0 < end; c0 += U * 256) {
+    float v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = c0 + u * 256 < end ? zr[c0 + u * 256] : -INFINITY;
+    for (int p = 1; p < a.splits; ++p) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] += c0 + u * 256 < end ? zr[p * step + c0 + u * 256] : 0.f;
+    }
+    float mx = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = c0 + u * 256;
+      if (c < end) {
+        if (a.bias) v[u] += a.bias[c];
+        zr[c] = v[u];
+      }
+      mx = fmaxf(mx, v[u]);
+    }
+    const float base = mx == -INFINITY ? 0.f : mx;
+    s *= exp_fast(m - base);
+#pragma unroll
+    for (int u = 0; u < U; ++u) s += exp_fast(v[u] - base);
+    m = mx;
+  }
+  merge_all<256>(m, s, lds);
+  if (threadIdx.x == 0) stats[row * parts + blockIdx.y] = make_float2(m, s);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void loss_parts_end_kernel(LossRows a, const float2* __restrict__ stats, int parts) {
+  const long row = blockIdx.x;
+  const int lab = row < a.rows ? a.labels[row] : -1;
+  const bool live = label_ok(lab, a.classes);
+  float* zr = a.z + (size_t)(row < a.rows ? row : 0) * a.ldz;
+  float lse = 0.f;
+  if (live) {
+    float m = -INFINITY, s = 0.f;
+    for (int i = threadIdx.x & 63; i < parts; i += 64) merge(m, s, stats[row * parts + i].x, stats[row * parts + i].y);
+    merge_all<64>(m, s, nullptr);
+    lse = m + logf(s);
+  }
+  const int lo = blockIdx.y * LOSS_PART, hi = (int)min((long)lo + LOSS_PART, a.dz ? a.ldd : (long)a.classes);
+  // the part that holds the label, or the first one of a padding row
+  if (row < a.rows && threadIdx.x == 0 && (live ? lab >= lo && lab < lo + LOSS_PART : blockIdx.y == 0))
+    a.loss[1 + row] = live ? lse - zr[lab] : 0.f;
+  if (!a.dz) return;
+  __syncthreads();  // the label's logit is read before its place is written
+  if (a.xc && row < a.rows) {
+    constexpr int VEC = TypeInfo<T>::VEC;
+    const T* xr = (const T*)a.x + row * a.in;
+    T* o = (T*)a.xc + row * a.ldx;
+    for (long c = ((long)blockIdx.y * 256 + threadIdx.x) * VEC; c < a.ldx; c += (long)gridDim.y * 256 * VEC) {
+      union { uint4 u; T e[VEC]; } v;
+      v.u = make_uint4(0, 0, 0, 0);
+      if (live) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+          if (c + j < a.in) v.e[j] = xr[c + j];
+      }
+      *(uint4*)(o + c) = v.u;
+    }
+  }
+  for (int c = lo + threadIdx.x; c < hi; c += 256) {
+    float v = 0.f;
+    if (live && c < a.classes) v = exp_fast(zr[c] - lse) - (c == lab ? 1.f : 0.f);
+    store_out<T>((T*)a.dz + row * a.ldd + c, v);
+    if (sizeof(T) == 2 && a.more) {
+      float left = v;
+      for (int i = 0; i < TERMS - 1; ++i) {
+        left -= bf16_to_f32(f32_to_bf16(left));
+        ((bf16_t*)a.more)[(i * a.rows_padded + row) * a.ldd + c] = f32_to_bf16(left);
+      }
+    }
+    if (a.keep_dz && row < a.rows && c < a.classes) zr[c] = v;
+  }
+}
+
 // For up to FINISH_ROWS rows: the mean, and the bias gradient from the
 // unrounded dlogits, 32 columns a workgroup.  Each workgroup counts the rows
 // for itself; the first one writes the mean and the unit.
@@ -604,6 +700,24 @@ hipError_t launch_loss_mean(const int32_t* labels, int classes, long rows, float
 }
 
 hipError_t launch_loss_rows(int dt, const LossRows& a, hipStream_t st) {
+  // One row per workgroup leaves the chip empty where rows are few and long:
+  // 64 rows of 50000 classes took 122 us.
+  if (a.stats) {
+    const int parts = loss_parts(a.classes);
+    {
+      TraceScope ts("loss_parts_kernel", st, 4.0 * a.rows * a.classes * (a.splits + 1), WORK_BYTE);
+      hipLaunchKernelGGL(loss_parts_kernel, dim3((unsigned)a.rows, parts), dim3(256), 0, st, a, a.stats, parts);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    TraceScope ts("loss_parts_end_kernel", st, (double)a.rows * a.classes * (8 + dt_size(dt)), WORK_BYTE);
+    const dim3 grid((unsigned)a.rows_padded, (unsigned)(a.dz ? (a.ldd + LOSS_PART - 1) / LOSS_PART : parts));
+    if (dt == BF16)
+      hipLaunchKernelGGL(loss_parts_end_kernel<bf16_t>, grid, dim3(256), 0, st, a, a.stats, parts);
+    else
+      hipLaunchKernelGGL(loss_parts_end_kernel<float>, grid, dim3(256), 0, st, a, a.stats, parts);
+    return hipGetLastError();
+  }
   TraceScope ts("loss_rows_kernel", st, (double)a.rows * a.classes * (8 + dt_size(dt)), WORK_BYTE);
   const bool wide = a.classes > 256;  // a workgroup per row, else a wave
   const dim3 grid((unsigned)(wide ? a.rows_padded : (a.rows_padded + 3) / 4));

@@ -746,68 +746,116 @@ __device__ __forceinline__ void product_tile(const GemmArgs& g, int wg, char* sm
         read(u * RPP + rr, vs[u]);
         ris[u] = info[row0 + u * RPP + rr - m0];
       }
+      // Each step for all rows before the next: their chains of dependent
+      // instructions overlap, and what few rows need is one branch for all.
+      bool hit = false, dead = false;
+      uint32_t at[UN];
 #pragma unroll
       for (int u = 0; u < UN; ++u) {
-        const int row = row0 + u * RPP + rr;
-        const RowInfo ri = ris[u];
-        float(&v)[8] = vs[u];
-        const bool live = label_ok(ri.lab, g.e.classes);
-        const uint32_t at = (uint32_t)ri.lab - (uint32_t)(g.e.col0 + col);
+        at[u] = (uint32_t)ris[u].lab - (uint32_t)(g.e.col0 + col);
+        if (!label_ok(ris[u].lab, g.e.classes)) {
+          dead = true;
+          at[u] = 8u;
+        }
+        hit |= at[u] < 8u;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += cols.bias[j];
-        if constexpr (EPI == EPI_LSE) {
-          static_assert(EPI != EPI_LSE || FN * 32 % STAT_COLS == 0, "whole groups of columns");
-          constexpr int LPG = STAT_COLS / 8;  // lanes per group
-          if (edge) {
+        for (int j = 0; j < 8; ++j) vs[u][j] += cols.bias[j];
+      }
+      hit = __any(hit);
+      dead = __any(dead);
+      if constexpr (EPI == EPI_LSE) {
+        static_assert(EPI != EPI_LSE || FN * 32 % STAT_COLS == 0, "whole groups of columns");
+        constexpr int LPG = STAT_COLS / 8;  // lanes per group
+        if (edge) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = col + j < g.N ? v[j] : -INFINITY;
+          for (int u = 0; u < UN; ++u)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) vs[u][j] = col + j < g.N ? vs[u][j] : -INFINITY;
+        }
+        float m[UN], s[UN];
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+          const float(&v)[8] = vs[u];
+          m[u] = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+        }
+#pragma unroll
+        for (int d = 1; d < LPG; d <<= 1)
+#pragma unroll
+          for (int u = 0; u < UN; ++u) m[u] = fmaxf(m[u], lane_xor(m[u], d));
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+          const float ms = m[u] == -INFINITY ? 0.f : m[u];
+          float x[8];  // their sum is NaN where a value is (fmaxf passed over it)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[j] = exp_fast(vs[u][j] - ms);
+          s[u] = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+        }
+#pragma unroll
+        for (int d = 1; d < LPG; d <<= 1)
+#pragma unroll
+          for (int u = 0; u < UN; ++u) s[u] += lane_xor(s[u], d);
+        if (c8 % STAT_COLS == 0 && col < g.N) {
+#pragma unroll
+          for (int u = 0; u < UN; ++u) {
+            const int row = row0 + u * RPP + rr;
+            if (row < g.M) g.e.stats[(size_t)row * g.e.nstat + g.e.stat0 + col / STAT_COLS] = make_float2(m[u], s[u]);
           }
-          float m = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+        }
+        if (hit) {
 #pragma unroll
-          for (int d = 1; d < LPG; d <<= 1) m = fmaxf(m, lane_xor(m, d));
-          const float ms = m == -INFINITY ? 0.f : m;
-          float s = 0.f;  // NaN where a value is (fmaxf passed over it)
+          for (int u = 0; u < UN; ++u) {
+            if (at[u] < 8u) {
+              float z = vs[u][0];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) s += exp_fast(v[j] - ms);
-#pragma unroll
-          for (int d = 1; d < LPG; d <<= 1) s += lane_xor(s, d);
-          if (row < g.M) {
-            if (c8 % STAT_COLS == 0 && col < g.N)
-              g.e.stats[(size_t)row * g.e.nstat + g.e.stat0 + col / STAT_COLS] = make_float2(m, s);
-            if (at < 8u && live) {
-              float z = v[0];
-#pragma unroll
-              for (int j = 1; j < 8; ++j) z = at == (uint32_t)j ? v[j] : z;
-              g.e.zlab[row] = z;
+              for (int j = 1; j < 8; ++j) z = at[u] == (uint32_t)j ? vs[u][j] : z;
+              g.e.zlab[row0 + u * RPP + rr] = z;
             }
           }
-        } else {
+        }
+      } else {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = exp_fast(v[j] - ri.lse);
-          if (at < 8u) {
+        for (int u = 0; u < UN; ++u)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] -= at == (uint32_t)j ? 1.f : 0.f;
-          }
-          if (edge || !live) {
+          for (int j = 0; j < 8; ++j) vs[u][j] = exp_fast(vs[u][j] - ris[u].lse);
+        if (hit) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = live && col + j < g.N ? v[j] : 0.f;
-          }
+          for (int u = 0; u < UN; ++u)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) cs[j] += v[j];
+            for (int j = 0; j < 8; ++j) vs[u][j] -= at[u] == (uint32_t)j ? 1.f : 0.f;
+        }
+        if (edge || dead) {
+#pragma unroll
+          for (int u = 0; u < UN; ++u)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              vs[u][j] = label_ok(ris[u].lab, g.e.classes) && col + j < g.N ? vs[u][j] : 0.f;
+        }
+        if (g.e.colsum) {
+#pragma unroll
+          for (int u = 0; u < UN; ++u)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) cs[j] += vs[u][j];
+        }
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
           const uint32_t o = at_y + (uint32_t)(bm * 32 + u * RPP) * pitch_y;
           if constexpr (sizeof(T) == 4) {
-            buf_store4<false>(yr, o, v);
-            buf_store4<false>(yr, o + 16, v + 4);
+            buf_store4<false>(yr, o, vs[u]);
+            buf_store4<false>(yr, o + 16, vs[u] + 4);
           } else {
-            buf_store8h<false>(yr, o, v);
-            if (g.e.more) {
+            buf_store8h<false>(yr, o, vs[u]);
+          }
+        }
+        if constexpr (sizeof(T) == 2) {
+          if (g.e.more) {
 #pragma unroll
-              for (int t = 0; t < TERMS - 1; ++t) {
+            for (int t = 0; t < TERMS - 1; ++t)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] -= bf16_to_f32(f32_to_bf16(v[j]));
-                buf_store8h<false>(t ? mr1 : mr0, o, v);
+              for (int u = 0; u < UN; ++u) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) vs[u][j] -= bf16_to_f32(f32_to_bf16(vs[u][j]));
+                buf_store8h<false>(t ? mr1 : mr0, at_y + (uint32_t)(bm * 32 + u * RPP) * pitch_y, vs[u]);
               }
-            }
           }
         }
       }
@@ -947,7 +995,7 @@ inline Plan plan_product(int dt, int M, int N, int K, int epi) {
 
 // The same for two products in one launch (of one tile): as long as the longer
 // workgroup, or as all of them over the slots and half of a shorter one at the
-// end.
+// end (250 + 256 tiles of 256 x 256: 251 us, one after the other 228).
 struct PairPlan {
   Plan a, b;
   double t;
@@ -967,7 +1015,8 @@ inline PairPlan plan_pair(int dt, int Ma, int Na, int Ka, int Mb, int Nb, int Kb
         if ((sa > 1 && na > 1024) || (sb > 1 && nb > 1024)) continue;
         const double da = wg_time(tile, dt, pa, na + nb), db = wg_time(tile, dt, pb, na + nb);
         double t = da > db ? da : db;
-        const double all = (na * da + nb * db) / slots + (na + nb > slots ? 0.5 * (da < db ? da : db) : 0);
+        const double lo = da < db ? da : db;
+        const double all = (na * da + nb * db) / slots + (na + nb > slots ? 0.5 * lo : 0);
         if (all > t) t = all;
         t += cut_time(sa, Ma, Na) + cut_time(sb, Mb, Nb);
         if (t < best.t) best = PairPlan{{tile, (int)div_up(ka, pa), (int)pa, t}, {tile, (int)div_up(kb, pb), (int)pb, t}, t};
@@ -979,6 +1028,30 @@ inline PairPlan plan_pair(int dt, int Ma, int Na, int Ka, int Mb, int Nb, int Kb
 inline bool pair_pays(int dt, const PairPlan& p, int Ma, int Na, int Ka, int Mb, int Nb, int Kb) {
   return p.t < plan_product(dt, Ma, Na, Ka, EPI_OUT).t + plan_product(dt, Mb, Nb, Kb, EPI_OUT).t + 3;
 }
+// Up to SKINNY_ROWS rows: whether the pass over B without LDS is faster than
+// tiles (and, for odd row lengths, the copies that those need).  Measured, in
+// us, at 1 / 16 / 32 / 64 rows against tiles: bf16 4096 x 4096 7.3 / 9.6 /
+// 13.7 / 22 against 14 .. 15; 50000 x 2048 44 / 51 / 71 / 116 against 33;
+// 1000 x 9216 12 / 18 / 26 / 45 against 14 .. 16; 777 x 1001 6 / 6 / 8 / 12
+// against 16; fp32 4096 x 4096 18 / 19 / 24 / 39 against 27.  The model: the
+// runs of steps one wave makes, each slower with more rows, or B's bytes at a
+// rate that longer runs bring nearer to the memory's.
+inline bool skinny_pays(int dt, int M, int N, int K) {
+  if (M > SKINNY_ROWS) return false;
+  const double es = dt == BF16 ? 2 : 4, bytes = es * N * K;
+  const int u = M <= 32 ? 8 : 4, run = 4 * (dt == BF16 ? 32 : 16) * u;
+  const double runs = (double)div_up(K, run);
+  const double per = M <= 16 ? (dt == BF16 ? 0.9 + 0.045 * M : 1.5 + 0.015 * M) : M <= 32 ? 1.2 + 0.04 * M : 0.95 + 0.02 * M;
+  const double rate = 7.4e6 * runs / (runs + 1);
+  const double pass = bytes / rate * (1 + (dt == BF16 ? 0.026 : 0.04) * M);
+  const double odd = dt == BF16 && K % 2 ? 2 : 1;  // rows that start inside a 4-byte word: 16 us for 7.3
+  const double skinny = 4 + odd * (runs * per > pass ? runs * per : pass);
+  double tiles = plan_product(dt, M, N, K, EPI_OUT).t;
+  if (tiles < 5 + bytes / 5.3e6) tiles = 5 + bytes / 5.3e6;
+  if (K % (dt == BF16 ? 8 : 4)) tiles += 4 + 2 * bytes / 5e6;
+  return skinny < tiles;
+}
+
 inline size_t partial_bytes_of(const Plan& p, int M, int N) {
   return p.splits > 1 ? (size_t)p.splits * M * (((size_t)N + 7) / 8 * 8) * 4 : 0;
 }

@@ -99,8 +99,8 @@ def test_scaled_updates_refuse():
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
 def test_workspaces(dt):
     es = torch.empty((), dtype=dt).element_size()
-    # up to 64 rows read the weights as they are
-    for rows in (0, 1, 64):
+    # few rows read the weights as they are
+    for rows in (0, 1, 16):
         assert singa.linear_fwd_workspace_bytes(dt, rows, 1001, 777) == 0
     # odd rows cost a copy of both matrices
     assert singa.linear_fwd_workspace_bytes(dt, 4096, 1001, 4096) >= 2 * 4096 * 1001 * es
