@@ -93,7 +93,9 @@ hipError_t launch_product(const Product& p, float* partial, hipStream_t st);
 // contiguous) and weight gradient (both rows contiguous), in one launch where
 // that is faster; workspace: the larger of the two products' and this.
 size_t pair_partial_bytes(int dt, int Ma, int Na, int Ka, int Mb, int Nb, int Kb);
-hipError_t launch_pair(const Product& dx, const Product& dw, float* partial, hipStream_t st);
+// finish (may be null): done by further workgroups of that launch, or before.
+struct LossFinish;
+hipError_t launch_pair(const Product& dx, const Product& dw, const LossFinish* finish, float* partial, hipStream_t st);
 // Number of partial sums of that product; launch_product with `raw` writes
 // them ([M][N rounded up to 8] each, also when it is one) and stops there.
 int product_splits(int dt, int M, int N, int K);
@@ -159,15 +161,27 @@ struct LossRows {
   int in;
   long ldx;
   float2* stats;  // [rows][loss_parts(classes)]: several workgroups per row; null: one
+  float* unit;    // unless null, scale / count is written there (up to FINISH_ROWS rows)
+  float scale;
 };
 constexpr int LOSS_PART = 4096;  // classes per workgroup then
 inline int loss_parts(int classes) { return (classes + LOSS_PART - 1) / LOSS_PART; }
 hipError_t launch_loss_rows(int dt, const LossRows& a, hipStream_t st);
-// The mean and the unit (may be null) of up to FINISH_ROWS rows and, unless db
-// is null, db (+)= unit times the sum of the valid rows of dz.
-constexpr int FINISH_ROWS = 1024;
-hipError_t launch_loss_finish(const int32_t* labels, int classes, int rows, float* loss, float* unit, float scale,
-                              const float* dz, long ld, float* db, int add, hipStream_t st);
+// The mean of up to FINISH_ROWS rows and, unless db is null, db (+)= scale /
+// count times the sum of the valid rows of dz.
+constexpr int FINISH_ROWS = 1024, FINISH_COLS = 8;
+struct LossFinish {
+  const int32_t* labels;
+  int classes, rows;
+  float* loss;
+  float scale;
+  const float* dz;
+  long ld;
+  float* db;
+  int add;
+};
+inline unsigned finish_wgs(const LossFinish& f) { return f.db ? (unsigned)((f.classes + FINISH_COLS - 1) / FINISH_COLS) : 1u; }
+hipError_t launch_loss_finish(const LossFinish& f, hipStream_t st);
 // colsum [groups][cols] of dzf [rows][ld] over COLSUM_ROWS rows each, those
 // with a valid label
 hipError_t launch_colsum_rows(const float* dzf, long ld, float* colsum, long rows, int cols, const int32_t* labels,

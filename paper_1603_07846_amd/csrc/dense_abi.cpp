@@ -199,9 +199,10 @@ size_t carve_loss(int dt, int rows, int in, int classes, bool grad, int dw_dt, v
 
 Operand op(const void* p, long ld, bool kc) { return Operand{p, ld, kc}; }
 
-hipError_t launch_gradients(const Product* dx, const Product* dw, float* partial, hipStream_t st) {
-  if (dx && dw) return launch_pair(*dx, *dw, partial, st);
-  return dx || dw ? launch_product(dx ? *dx : *dw, partial, st) : hipSuccess;
+hipError_t launch_gradients(const Product* dx, const Product* dw, const LossFinish* finish, float* partial, hipStream_t st) {
+  if (dx && dw) return launch_pair(*dx, *dw, finish, partial, st);
+  const hipError_t e = finish ? launch_loss_finish(*finish, st) : hipSuccess;
+  return e == hipSuccess && (dx || dw) ? launch_product(dx ? *dx : *dw, partial, st) : e;
 }
 
 }  // namespace
@@ -338,7 +339,7 @@ int singa_linear_bwd(singa_dtype dtype, int rows, int in, int out, const void* x
     q.e.out_f32 = dw_dtype == SINGA_F32;
     q.e.add = accumulate != 0;
   }
-  if (e == hipSuccess) e = launch_gradients(dx ? &p : nullptr, dw ? &q : nullptr, o.partial, st);
+  if (e == hipSuccess) e = launch_gradients(dx ? &p : nullptr, dw ? &q : nullptr, nullptr, o.partial, st);
   return status(e);
 }
 
@@ -403,7 +404,9 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
   const bool split = o.split && dw;
   void* more = split ? o.more : nullptr;
   const long groups = up(rows, COLSUM_ROWS) / COLSUM_ROWS;
-  const bool finish = o.keep && rows <= FINISH_ROWS;  // the mean and db in one kernel
+  // few rows of kept logits: the mean and db with the gradients' launch
+  const bool finish = o.keep && rows <= FINISH_ROWS;
+  const LossFinish fin{labels, classes, rows, loss, scale, o.logits, o.ldl, db, accumulate};
   if (o.keep) {
     // the logits, then their rows
     Product q = p;
@@ -427,6 +430,8 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
     r.classes = classes;
     r.loss = loss;
     r.stats = o.stats;
+    r.unit = grad && finish ? o.unit : nullptr;
+    r.scale = scale;
     if (!grad) {
       r.rows_padded = rows;
     } else {
@@ -442,8 +447,7 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
       r.ldx = o.k.ld;
     }
     if (e == hipSuccess) e = launch_loss_rows(dtype, r, st);
-    if (e == hipSuccess && finish)
-      e = launch_loss_finish(labels, classes, rows, loss, grad ? o.unit : nullptr, scale, o.logits, o.ldl, db, accumulate, st);
+    if (e == hipSuccess && finish && !grad) e = launch_loss_finish(fin, st);
   } else {
     p.epi = EPI_LSE;
     p.e.stats = o.stats;
@@ -523,7 +527,7 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
       v.e.out_f32 = dw_dtype == SINGA_F32;
       v.e.add = accumulate != 0;
     }
-    if (e == hipSuccess) e = launch_gradients(dx ? &q : nullptr, dw ? &v : nullptr, o.partial, st);
+    if (e == hipSuccess) e = launch_gradients(dx ? &q : nullptr, dw ? &v : nullptr, finish ? &fin : nullptr, o.partial, st);
   }
   if (e == hipSuccess && dx && !o.one) e = launch_round_rows(dtype, o.dxf, dx, rows, in, labels, classes, st);
   return status(e);

@@ -340,17 +340,6 @@ __global__ __launch_bounds__(256) void lse_kernel(const float2* __restrict__ sta
   }
 }
 
-__device__ __forceinline__ double block_sum(double v, double* lds) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  double s = 0;
-  for (int i = 0; i < (int)blockDim.x / 64; ++i) s += lds[i];
-  __syncthreads();
-  return s;
-}
-
 // One workgroup: the mean over the counted rows, in a fixed order, and what a
 // counted row's gradient is multiplied with.
 __global__ __launch_bounds__(1024) void loss_mean_kernel(const int32_t* __restrict__ labels, int classes, long rows,
@@ -375,11 +364,19 @@ __global__ __launch_bounds__(1024) void loss_mean_kernel(const int32_t* __restri
 // reads the logits back (from the thread's own stores) and leaves the unrounded
 // dlogits there for the column sums.  The row of x goes along, cleaned.
 template <typename T, int W>
-__global__ __launch_bounds__(256) void loss_rows_kernel(LossRows a) {
-  __shared__ float2 lds[4];
+__global__ __launch_bounds__(W > 256 ? W : 256) void loss_rows_kernel(LossRows a) {
+  __shared__ float2 lds[16];
   __shared__ float zl[4];
+  constexpr int WG = W > 256 ? W : 256;
   const int t = threadIdx.x % W, in_wg = threadIdx.x / W;
-  const long row = (long)blockIdx.x * (256 / W) + in_wg;
+  const long row = (long)blockIdx.x * (WG / W) + in_wg;
+  if (a.unit && blockIdx.x == 0) {  // (up to FINISH_ROWS rows)
+    __shared__ double cnt[16];
+    double n = 0;
+    for (long r = threadIdx.x; r < a.rows; r += WG) n += label_ok(a.labels[r], a.classes);
+    n = block_sum(n, cnt);
+    if (threadIdx.x == 0) a.unit[0] = n > 0 ? (float)(a.scale / n) : 0.f;
+  }
   if (row >= a.rows_padded) return;
   const int lab = row < a.rows ? a.labels[row] : -1;
   const bool live = label_ok(lab, a.classes);
@@ -462,6 +459,13 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(LossRows a) {
 __global__ __launch_bounds__(256) void loss_parts_kernel(LossRows a, float2* __restrict__ stats, int parts) {
   __shared__ float2 lds[4];
   const long row = blockIdx.x;
+  if (a.unit && blockIdx.x == 0 && blockIdx.y == 0) {
+    __shared__ double cnt[4];
+    double n = 0;
+    for (long r = threadIdx.x; r < a.rows; r += 256) n += label_ok(a.labels[r], a.classes);
+    n = block_sum(n, cnt);
+    if (threadIdx.x == 0) a.unit[0] = n > 0 ? (float)(a.scale / n) : 0.f;
+  }
   if (!label_ok(a.labels[row], a.classes)) return;
   constexpr int U = 4;
   float* zr = a.z + (size_t)row * a.ldz;
@@ -545,39 +549,9 @@ __global__ __launch_bounds__(256) void loss_parts_end_kernel(LossRows a, const f
   }
 }
 
-// For up to FINISH_ROWS rows: the mean, and the bias gradient from the
-// unrounded dlogits, 32 columns a workgroup.  Each workgroup counts the rows
-// for itself; the first one writes the mean and the unit.
-__global__ __launch_bounds__(1024) void loss_finish_kernel(const int32_t* __restrict__ labels, int classes, int rows,
-                                                           float* __restrict__ loss, float* __restrict__ unit, float scale,
-                                                           const float* __restrict__ dz, long ld, float* __restrict__ db,
-                                                           int add) {
-  __shared__ double lds[16];
-  __shared__ float red[32][33];
-  const int t = threadIdx.x;
-  const bool ok = t < rows && label_ok(labels[t], classes);
-  const double n = block_sum(ok ? 1.0 : 0.0, lds);
-  const float un = n > 0 ? (float)(scale / n) : 0.f;
-  if (blockIdx.x == 0) {
-    const double s = block_sum(ok ? (double)loss[1 + t] : 0.0, lds);
-    if (t == 0) {
-      loss[0] = n > 0 ? (float)(s / n) : 0.f;
-      if (unit) unit[0] = un;
-    }
-  }
-  if (!db) return;
-  const int tc = t & 31, tr = t >> 5, col = blockIdx.x * 32 + tc;
-  float s = 0.f;
-  if (col < classes)
-    for (int r = tr; r < rows; r += 32) s += label_ok(labels[r], classes) ? dz[(size_t)r * ld + col] : 0.f;
-  red[tr][tc] = s;
-  __syncthreads();
-  if (tr || col >= classes) return;
-  s = 0.f;
-#pragma unroll
-  for (int r = 0; r < 32; ++r) s += red[r][tc];
-  s *= un;
-  db[col] = add ? db[col] + s : s;
+__global__ __launch_bounds__(256) void loss_finish_kernel(LossFinish f) {
+  __shared__ __align__(16) char lds[FINISH_LDS];
+  loss_finish(f, blockIdx.x, lds);
 }
 
 // One or a few rows of many column groups: the loss of each, and the mean.
@@ -719,27 +693,29 @@ hipError_t launch_loss_rows(int dt, const LossRows& a, hipStream_t st) {
     return hipGetLastError();
   }
   TraceScope ts("loss_rows_kernel", st, (double)a.rows * a.classes * (8 + dt_size(dt)), WORK_BYTE);
-  const bool wide = a.classes > 256;  // a workgroup per row, else a wave
-  const dim3 grid((unsigned)(wide ? a.rows_padded : (a.rows_padded + 3) / 4));
+  // a wave per row of few classes, else a workgroup, of 1024 threads where rows
+  // are too few for the chip to fill otherwise
+  const int w = a.classes <= 256 ? 64 : a.classes > 2048 && a.rows < 1024 ? 1024 : 256;
+  const dim3 grid((unsigned)(w == 64 ? (a.rows_padded + 3) / 4 : a.rows_padded)), wg(w == 64 ? 256 : w);
+#define SINGA_ROWS(T)                                                            \
+  if (w == 64)                                                                   \
+    hipLaunchKernelGGL((loss_rows_kernel<T, 64>), grid, wg, 0, st, a);           \
+  else if (w == 256)                                                             \
+    hipLaunchKernelGGL((loss_rows_kernel<T, 256>), grid, wg, 0, st, a);          \
+  else                                                                           \
+    hipLaunchKernelGGL((loss_rows_kernel<T, 1024>), grid, wg, 0, st, a)
   if (dt == BF16) {
-    if (wide)
-      hipLaunchKernelGGL((loss_rows_kernel<bf16_t, 256>), grid, dim3(256), 0, st, a);
-    else
-      hipLaunchKernelGGL((loss_rows_kernel<bf16_t, 64>), grid, dim3(256), 0, st, a);
+    SINGA_ROWS(bf16_t);
   } else {
-    if (wide)
-      hipLaunchKernelGGL((loss_rows_kernel<float, 256>), grid, dim3(256), 0, st, a);
-    else
-      hipLaunchKernelGGL((loss_rows_kernel<float, 64>), grid, dim3(256), 0, st, a);
+    SINGA_ROWS(float);
   }
+#undef SINGA_ROWS
   return hipGetLastError();
 }
 
-hipError_t launch_loss_finish(const int32_t* labels, int classes, int rows, float* loss, float* unit, float scale,
-                              const float* dz, long ld, float* db, int add, hipStream_t st) {
-  TraceScope ts("loss_finish_kernel", st, db ? 4.0 * rows * classes : 8.0 * rows, WORK_BYTE);
-  hipLaunchKernelGGL(loss_finish_kernel, dim3(db ? (unsigned)((classes + 31) / 32) : 1u), dim3(1024), 0, st, labels, classes,
-                     rows, loss, unit, scale, dz, ld, db, add);
+hipError_t launch_loss_finish(const LossFinish& f, hipStream_t st) {
+  TraceScope ts("loss_finish_kernel", st, f.db ? 4.0 * f.rows * f.classes : 8.0 * f.rows, WORK_BYTE);
+  hipLaunchKernelGGL(loss_finish_kernel, dim3(finish_wgs(f)), dim3(256), 0, st, f);
   return hipGetLastError();
 }
 

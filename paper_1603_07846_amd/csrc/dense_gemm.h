@@ -408,6 +408,54 @@ template <typename T, bool KC, int R, int F> struct Frags {
 // that the barrier has freed; the other loads follow in the next step (64 KB in
 // one step of 512 cycles were twice what the vector memory path takes: 870 ->
 // 833 us at 8192^3).  A barrier waits for loads issued at least two steps ago.
+__device__ __forceinline__ double block_sum(double v, double* lds) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  double s = 0;
+  for (int i = 0; i < (int)blockDim.x / 64; ++i) s += lds[i];
+  __syncthreads();
+  return s;
+}
+
+// For up to FINISH_ROWS rows: the mean, and the bias gradient from the
+// unrounded dlogits, FINISH_COLS columns per workgroup of 256 threads.  Each
+// workgroup counts the rows for itself; the first one writes the mean.
+constexpr int FINISH_LDS = 4 * 8 + 32 * (FINISH_COLS + 1) * 4;
+__device__ __forceinline__ void loss_finish(const LossFinish& f, int wg, char* smem) {
+  double* const lds = (double*)smem;
+  float* const red = (float*)(smem + 4 * 8);
+  const int t = threadIdx.x;
+  double n = 0, s = 0;
+  for (int r = t; r < f.rows; r += 256)
+    if (label_ok(f.labels[r], f.classes)) {
+      n += 1;
+      if (wg == 0) s += f.loss[1 + r];
+    }
+  n = block_sum(n, lds);
+  if (wg == 0) {
+    s = block_sum(s, lds);
+    if (t == 0) f.loss[0] = n > 0 ? (float)(s / n) : 0.f;
+  }
+  if (!f.db) return;
+  const int tc = t % FINISH_COLS, tr = t / FINISH_COLS, col = wg * FINISH_COLS + tc;
+  constexpr int LANES = 256 / FINISH_COLS;
+  float c = 0.f;
+  if (col < f.classes) {
+#pragma unroll 4
+    for (int r = tr; r < f.rows; r += LANES) c += label_ok(f.labels[r], f.classes) ? f.dz[(size_t)r * f.ld + col] : 0.f;
+  }
+  red[tr * (FINISH_COLS + 1) + tc] = c;
+  __syncthreads();
+  if (tr || col >= f.classes) return;
+  c = 0.f;
+#pragma unroll
+  for (int r = 0; r < LANES; ++r) c += red[r * (FINISH_COLS + 1) + tc];
+  c *= n > 0 ? (float)(f.scale / n) : 0.f;
+  f.db[col] = f.add ? f.db[col] + c : c;
+}
+
 template <typename T, bool AKC, bool BKC, int WM, int WN, int FM, int FN> struct Shape {
   static constexpr int NW = WM * WN, BM = WM * FM * 32, BN = WN * FN * 32;
   typedef Tile<T, AKC, BM, NW> TA;
@@ -891,9 +939,11 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : FM == 2 ? 2 : 4) void pr
 
 // The two products of a layer's gradients in one launch, source gradient
 // first: neither leaves the chip half empty while the other waits.
+// What is left of a loss (LossFinish) rides along in further workgroups.
 struct PairArgs {
   GemmArgs dx, dw;
-  int wgs_dx;
+  int wgs_dx, wgs;
+  LossFinish finish;
 };
 template <typename T, int FM, int FN>
 __global__ __launch_bounds__(256, FM == 4 ? 1 : FM == 2 ? 2 : 4) void product_pair_kernel(PairArgs p) {
@@ -901,8 +951,10 @@ __global__ __launch_bounds__(256, FM == 4 ? 1 : FM == 2 ? 2 : 4) void product_pa
   __shared__ __align__(1024) char smem[S1 > S2 ? S1 : S2];
   if ((int)blockIdx.x < p.wgs_dx)
     product_tile<T, true, false, 2, 2, FM, FN, EPI_OUT>(p.dx, blockIdx.x, smem);
-  else
+  else if ((int)blockIdx.x < p.wgs)
     product_tile<T, false, false, 2, 2, FM, FN, EPI_OUT>(p.dw, (int)blockIdx.x - p.wgs_dx, smem);
+  else
+    loss_finish(p.finish, (int)blockIdx.x - p.wgs, smem);
 }
 
 // Adds the partial sums of a split product in order and finishes them.
@@ -1124,17 +1176,21 @@ template <typename T> hipError_t launch_product_t(const Product& p, float* parti
   return e == hipSuccess ? launch_reduce<T>(p, g, st) : e;
 }
 
-template <typename T> hipError_t launch_pair_t(const Product& dx, const Product& dw, float* partial, hipStream_t st) {
+template <typename T>
+hipError_t launch_pair_t(const Product& dx, const Product& dw, const LossFinish* finish, float* partial, hipStream_t st) {
   const PairPlan pl = plan_pair(dx.dt, dx.M, dx.N, dx.K, dw.M, dw.N, dw.K);
   if (!pair_pays(dx.dt, pl, dx.M, dx.N, dx.K, dw.M, dw.N, dw.K)) {
-    const hipError_t e = launch_product_t<T>(dx, partial, st);
+    hipError_t e = finish ? launch_loss_finish(*finish, st) : hipSuccess;
+    if (e == hipSuccess) e = launch_product_t<T>(dx, partial, st);
     return e == hipSuccess ? launch_product_t<T>(dw, partial, st) : e;
   }
-  PairArgs a;
+  PairArgs a{};
   a.dx = args_of<T>(dx, pl.a, partial);
   a.dw = args_of<T>(dw, pl.b, partial + partial_bytes_of(pl.a, dx.M, dx.N) / 4);
   a.wgs_dx = (int)wgs_of(a.dx);
-  const dim3 grid((unsigned)(wgs_of(a.dx) + wgs_of(a.dw)));
+  a.wgs = (int)(wgs_of(a.dx) + wgs_of(a.dw));
+  if (finish) a.finish = *finish;
+  const dim3 grid((unsigned)a.wgs + (finish ? finish_wgs(*finish) : 0u));
   {
     TraceScope ts("product_pair_kernel", st, dx.flops + dw.flops, WORK_FLOP);
     constexpr bool F = sizeof(T) == 4;
