@@ -1082,10 +1082,10 @@ inline bool pair_pays(int dt, const PairPlan& p, int Ma, int Na, int Ka, int Mb,
 }
 // Up to SKINNY_ROWS rows: whether the pass over B without LDS is faster than
 // tiles (and, for odd row lengths, the copies that those need).  Measured, in
-// us, at 1 / 16 / 32 / 64 rows against tiles: bf16 4096 x 4096 7.3 / 9.6 /
-// 13.7 / 22 against 14 .. 15; 50000 x 2048 44 / 51 / 71 / 116 against 33;
-// 1000 x 9216 12 / 18 / 26 / 45 against 14 .. 16; 777 x 1001 6 / 6 / 8 / 12
-// against 16; fp32 4096 x 4096 18 / 19 / 24 / 39 against 27.  The model: the
+// us, at 1 / 16 / 32 / 64 rows against tiles: bf16 4096 x 4096 6.8 / 9.1 /
+// 12.6 / 20 against 12 .. 15; 50000 x 2048 36 / 47 / 69 / 115 against 33;
+// 1000 x 9216 12 / 18 / 25 / 41 against 13 .. 17; 777 x 1001 5 / 6 / 8 / 12
+// against 16; fp32 4096 x 4096 17 / 20 / 23 / 39 against 26 .. 28.  The model: the
 // runs of steps one wave makes, each slower with more rows, or B's bytes at a
 // rate that longer runs bring nearer to the memory's.
 inline bool skinny_pays(int dt, int M, int N, int K) {
