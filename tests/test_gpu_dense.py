@@ -579,3 +579,22 @@ def test_refusals_on_the_gpu():
     with pytest.raises(singa.SingaError) as e:
         singa.linear_softmax_ce(x, w, labels, workspace=singa.empty((64,), torch.uint8, "cuda"))
     assert e.value.status == -4
+
+
+
+@pytest.mark.parametrize("rows", [3, 150])
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_activations_far_below_zero(dt, act, rows):
+    """Values that an activation nearly cancels keep their relative precision.  z is exact (one product of 1 and z).
+    gelu: the argument of erfc is rounded twice (relative 2 F, so 4 u^2 F in exp(-u^2), u^2 = z^2 / 2), its square and
+    the base-2 argument once each (2 u^2 F more); 2^-19 covers the exponential, the polynomial's 4.5e-7 or erfc's own
+    ulps.  silu: 2 |z| F of the exponential's argument and 2^-20 of the rest."""
+    T = DT[dt]
+    z = torch.linspace(-11, 9, rows * 64).view(rows, 64).to(T)
+    x, w = dev(z, T), dev(torch.eye(64), T)
+    y = singa.linear_fwd(x, w, act=act)
+    zr = x.double()
+    yr = zr * torch.special.erfc(-zr / math.sqrt(2)) / 2 if act == "gelu" else act64(zr, act)
+    off = (6 * zr.square() / 2 * F + 2.0 ** -19 if act == "gelu" else 2 * zr.abs() * F + 2.0 ** -20) * yr.abs()
+    within("y", y, yr, off + u_of(T) * (yr.abs() + off))
