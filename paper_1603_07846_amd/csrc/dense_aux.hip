@@ -48,7 +48,7 @@ template <typename T, bool ALIGNED> __device__ __forceinline__ typename Chunk<T>
 
 // Eight waves share the K range: of 4 / 8 / 16 they took, for one row, bf16
 // 4096 x 4096 7.4 / 6.9 / 7.1 us, 32000 x 4096 44.4 / 41.9 / 42.5, and fp32
-// 50000 x 2048 76.8 / 69 / 67.6 (4096 x 4096 16.8 / 15.8 / 12.4).
+// 50000 x 2048 76.8 / 69 / 67.6.
 constexpr int SKINNY_WAVES = 8;
 
 template <typename T, bool ALIGNED, int MT, int EPI>
@@ -68,8 +68,14 @@ __global__ __launch_bounds__(SKINNY_WAVES * 64) void skinny_kernel(const T* __re
   for (int m = 0; m < MT; ++m) acc[m] = f32x4v{0.f, 0.f, 0.f, 0.f};
   typedef typename Chunk<T>::type C;
   const int full = K / (STEP * U);  // runs of U whole steps
+  // Rows a multiple of 16 KB apart start in the same memory channels: with the
+  // chip full of workgroups, each starts at another run (one row, fp32 4096 x
+  // 4096 17.4 -> 11.2 us, bf16 4096 x 8192 18.5 -> 12.8; at other pitches that
+  // cost up to a quarter, 32000 x 4096 bf16 42 -> 52).
+  const int rot = (size_t)K * sizeof(T) % 16384 == 0 && N >= 4096 ? (int)(blockIdx.x % (unsigned)full) : 0;
   for (int it = wave; it < full; it += SKINNY_WAVES) {
-    const int k = it * STEP * U + kq * VEC;
+    const int run = it + rot < full ? it + rot : it + rot - full;
+    const int k = run * STEP * U + kq * VEC;
     C wc[U], xc[MT][U];
 #pragma unroll
     for (int u = 0; u < U; ++u) wc[u] = row_chunk<T, ALIGNED>(wr, k + u * STEP);

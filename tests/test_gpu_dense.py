@@ -598,3 +598,11 @@ def test_activations_far_below_zero(dt, act, rows):
     yr = zr * torch.special.erfc(-zr / math.sqrt(2)) / 2 if act == "gelu" else act64(zr, act)
     off = (6 * zr.square() / 2 * F + 2.0 ** -19 if act == "gelu" else 2 * zr.abs() * F + 2.0 ** -20) * yr.abs()
     within("y", y, yr, off + u_of(T) * (yr.abs() + off))
+
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 8, 24, 64])
+def test_few_rows_of_far_apart_weights(rows, dt):
+    """Rows of 16 and 32 KB, where the workgroups begin at different places of K."""
+    check_fwd(dt, rows, 8192, 4099, "none", True, False, False)
