@@ -17,7 +17,8 @@
  *     workspace, except in the pass over the weights that few rows take.
  *   - the workspace has no alignment but 16 bytes and needs no clearing; two
  *     calls whose execution may overlap need one each.
- *   - outputs may not overlap inputs unless stated.
+ *   - outputs may share memory with inputs or other outputs only where that is
+ *     stated (UNSUPPORTED).
  *   - sums are fp32 (norms fp64); bf16 outputs are rounded once, to nearest
  *     even.
  */
@@ -32,7 +33,7 @@ extern "C" {
 
 typedef enum {
   SINGA_ACT_NONE = 0,
-  SINGA_ACT_RELU = 1, /* z > 0 ? z : 0, derivative 0 at 0 */
+  SINGA_ACT_RELU = 1, /* z > 0 ? z : 0 (NaN stays), derivative 0 at 0 */
   SINGA_ACT_GELU = 2, /* z (1 + erf(z / sqrt 2)) / 2 */
   SINGA_ACT_SILU = 3  /* z / (1 + exp(-z)) */
 } singa_act;
@@ -44,7 +45,8 @@ typedef enum {
  *   z : dtype [rows][out] or NULL (written: what singa_linear_bwd needs)
  *   y : dtype [rows][out] (written), from the unrounded z
  * rows = 0 is a call without work.  in, out (here and below): 1 .. 2^20
- * each, rows at most 2^28 (UNSUPPORTED beyond).
+ * each, rows at most 2^28, a matrix (and rows x classes) at most 2^37 elements
+ * (UNSUPPORTED beyond).
  * Errors: NULL, SHAPE, UNSUPPORTED (dtype, act), ALIGN, WORKSPACE, HIP. */
 int singa_linear_fwd_workspace_bytes(singa_dtype dtype, int rows, int in, int out, size_t* bytes);
 int singa_linear_fwd(singa_dtype dtype, int rows, int in, int out, const void* x, const void* w, const float* bias,
@@ -118,7 +120,9 @@ int singa_grad_norm(int count, const int* dtypes, const void* const* grads, cons
                     float* stat, void* ws, size_t ws_bytes, singa_stream stream);
 
 /* The same, then out[i] = scale * grads[i] (rounded to the tensor's type);
- * out[i] == grads[i] clips in place, and then a scale of 1 writes nothing. */
+ * out[i] == grads[i] clips in place, and then a scale of 1 writes nothing.
+ * Outputs share memory with nothing else, so no gradient is listed twice
+ * (UNSUPPORTED). */
 int singa_grad_clip(int count, const int* dtypes, const void* const* grads, void* const* outs, const size_t* sizes,
                     float max_norm, float* stat, void* ws, size_t ws_bytes, singa_stream stream);
 

@@ -8,6 +8,8 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
+#include <memory>
+#include <new>
 
 #include "dense.h"
 #include "gradnorm.h"
@@ -25,6 +27,7 @@ bool dtype_ok(int dt) { return dt == SINGA_F32 || dt == SINGA_BF16; }
 constexpr int kMaxFeatures = 1 << 20;  // a row stays below 2^23 bytes, so 256 of them have 32-bit offsets
 
 constexpr int kMaxRows = 1 << 28;
+constexpr long kMaxMatrix = 1L << 37;  // elements of a matrix (or rows x classes): tiles and workgroups stay below 2^24
 
 // Hands out 256-byte aligned parts of a workspace (or, from NULL, counts them;
 // the first 256 bytes make up for a base that is only 16-byte aligned).
@@ -50,8 +53,31 @@ int check_ws(const void* ws, size_t have, size_t need) {
 int shape(int rows, int in, int out) {
   if (rows < 0 || in < 1 || out < 1) return SINGA_ERR_SHAPE;
   if (in > kMaxFeatures || out > kMaxFeatures || rows > kMaxRows) return SINGA_ERR_UNSUPPORTED;
+  if ((long)rows * in > kMaxMatrix || (long)rows * out > kMaxMatrix || (long)in * out > kMaxMatrix) return SINGA_ERR_UNSUPPORTED;
   return SINGA_OK;
 }
+
+// What a call reads or writes (NULL: nothing).
+struct Span {
+  const void* p;
+  size_t bytes;
+};
+bool apart(const Span& a, const Span& b) {
+  const uintptr_t pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
+  return !a.p || !b.p || pa + a.bytes <= pb || pb + b.bytes <= pa;
+}
+// Workgroups write outputs while others still read: no output may share memory
+// with an input or another output.
+template <int O, int I> int check_apart(const Span (&outs)[O], const Span (&ins)[I]) {
+  for (int i = 0; i < O; ++i) {
+    for (int j = 0; j < i; ++j)
+      if (!apart(outs[i], outs[j])) return SINGA_ERR_UNSUPPORTED;
+    for (const Span& in : ins)
+      if (!apart(outs[i], in)) return SINGA_ERR_UNSUPPORTED;
+  }
+  return SINGA_OK;
+}
+Span span(const void* p, long rows, long cols, int dt) { return {p, (size_t)rows * cols * dt_size(dt)}; }
 
 // The row length of a matrix kept in the workspace: rows a multiple of 4 KB
 // apart would all start in the same memory channel (a product over 32768 of k:
@@ -232,6 +258,10 @@ int singa_linear_fwd(singa_dtype dtype, int rows, int in, int out, const void* x
     return SINGA_ERR_ALIGN;
   FwdWs o;
   rc = check_ws(ws, ws_bytes, carve_fwd(dtype, rows, in, out, nullptr, &o));
+  if (rc == SINGA_OK)
+    rc = check_apart({span(y, rows, out, dtype), span(z, rows, out, dtype)},
+                     {span(x, rows, in, dtype), span(w, out, in, dtype), span(bias, 1, out, F32),
+                      span(residual == y ? nullptr : residual, rows, out, dtype)});
   if (rc != SINGA_OK) return rc;
   carve_fwd(dtype, rows, in, out, ws, &o);
   hipStream_t st = (hipStream_t)stream;
@@ -299,6 +329,11 @@ int singa_linear_bwd(singa_dtype dtype, int rows, int in, int out, const void* x
     if (e == hipSuccess && db) e = launch_zero(db, (size_t)out * 4, st);
     return status(e);
   }
+  rc = check_apart({span(dx, rows, in, dtype), span(dw, out, in, dw_dtype), span(db, 1, out, F32)},
+                   {span(dw ? x : nullptr, rows, in, dtype), span(dx ? w : nullptr, out, in, dtype), span(dy, rows, out, dtype),
+                    span(act == SINGA_ACT_NONE ? nullptr : z, rows, out, dtype),
+                    span(!dx || dx_residual == dx ? nullptr : dx_residual, rows, in, dtype)});
+  if (rc != SINGA_OK) return rc;
   BwdWs o;
   carve_bwd(dtype, rows, in, out, act, dw_dtype, ws, &o);
   const bool split = o.split && dw;
@@ -377,6 +412,11 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
     if (e == hipSuccess && db && !accumulate) e = launch_zero(db, (size_t)classes * 4, st);
     return status(e);
   }
+  rc = check_apart({{loss, (size_t)(rows + 1L) * 4}, span(dx, rows, in, dtype), span(dw, classes, in, dw_dtype),
+                    span(db, 1, classes, F32)},
+                   {span(x, rows, in, dtype), span(w, classes, in, dtype), span(bias, 1, classes, F32),
+                    span(labels, rows, 1, F32)});
+  if (rc != SINGA_OK) return rc;
   LossWs o;
   carve_loss(dtype, rows, in, classes, grad, dw_dtype, ws, &o);
   const void *xt = x, *wt = w;  // as the tiles take them
@@ -535,6 +575,32 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
 
 size_t singa_grad_norm_workspace_bytes(int count) { return count < 0 ? 0 : norm_slots(count) * sizeof(double); }
 
+// Clipping writes one tensor while it reads another: outputs may share memory
+// with nothing but the gradient they stand for (a gradient listed twice would
+// be scaled once or twice, as the workgroups happen to run).
+static int clip_apart(int count, const int* dtypes, const void* const* grads, void* const* outs, const size_t* sizes) {
+  struct Part {
+    uintptr_t lo, hi;
+    bool written;
+  };
+  const std::unique_ptr<Part[]> parts(new (std::nothrow) Part[2 * (size_t)count]);
+  if (!parts) return SINGA_ERR_HIP;
+  Part* end = parts.get();
+  for (int i = 0; i < count; ++i) {
+    if (!sizes[i]) continue;
+    const size_t bytes = sizes[i] * dt_size(dtypes[i]);
+    *end++ = {(uintptr_t)outs[i], (uintptr_t)outs[i] + bytes, true};
+    if (grads[i] != outs[i]) *end++ = {(uintptr_t)grads[i], (uintptr_t)grads[i] + bytes, false};
+  }
+  std::sort(parts.get(), end, [](const Part& a, const Part& b) { return a.lo < b.lo; });
+  uintptr_t read = 0, written = 0;  // the ends of what came before
+  for (const Part* p = parts.get(); p < end; ++p) {
+    if (p->lo < written || (p->written && p->lo < read)) return SINGA_ERR_UNSUPPORTED;
+    (p->written ? written : read) = std::max(p->written ? written : read, p->hi);
+  }
+  return SINGA_OK;
+}
+
 static int grad_norm(int count, const int* dtypes, const void* const* grads, void* const* outs, bool clip, const size_t* sizes,
                      float max_norm, float* stat, void* ws, size_t ws_bytes, singa_stream stream) {
   if (count < 0) return SINGA_ERR_SHAPE;
@@ -548,7 +614,8 @@ static int grad_norm(int count, const int* dtypes, const void* const* grads, voi
     if (!aligned_to(grads[i], dt_size(dtypes[i])) || (clip && !aligned_to(outs[i], dt_size(dtypes[i])))) return SINGA_ERR_ALIGN;
   }
   if (!aligned_to(stat, 4)) return SINGA_ERR_ALIGN;
-  const int rc = check_ws(ws, ws_bytes, singa_grad_norm_workspace_bytes(count));
+  int rc = check_ws(ws, ws_bytes, singa_grad_norm_workspace_bytes(count));
+  if (rc == SINGA_OK && clip && count) rc = clip_apart(count, dtypes, grads, outs, sizes);
   if (rc != SINGA_OK) return rc;
   return status(launch_grad_norm(count, dtypes, grads, clip ? outs : nullptr, sizes, max_norm, stat, (double*)ws,
                                  (hipStream_t)stream));

@@ -157,6 +157,14 @@ template <typename T> hipError_t skinny_t(const Product& p, hipStream_t st) {
   return aligned ? skinny_rows<T, true, EPI_LSE>(p, st) : skinny_rows<T, false, EPI_LSE>(p, st);
 }
 
+// A grid of one dimension holds 2^32 threads: many workgroups are dealt over
+// two.
+constexpr long GRID_X = 1 << 20;
+inline dim3 grid_of(long wgs) {
+  return wgs <= GRID_X ? dim3((unsigned)wgs) : dim3((unsigned)GRID_X, (unsigned)((wgs + GRID_X - 1) / GRID_X));
+}
+__device__ __forceinline__ long workgroup() { return (long)blockIdx.y * GRID_X + blockIdx.x; }
+
 // ------------------------------------------------------------ operands
 template <typename T>
 __global__ __launch_bounds__(256) void pack_kernel(const T* __restrict__ in, T* __restrict__ out, long rows,
@@ -164,7 +172,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const T* __restrict__ in, T* 
                                                    long ldo, const int32_t* __restrict__ labels, int classes) {
   constexpr int VEC = TypeInfo<T>::VEC;
   const long cpr = ldo / VEC;
-  const long i = (long)blockIdx.x * 256 + threadIdx.x;
+  const long i = workgroup() * 256 + threadIdx.x;
   if (i >= (rows + rows2) * cpr) return;
   long row = i / cpr;
   const long at = i - row * cpr;
@@ -295,7 +303,7 @@ __global__ __launch_bounds__(256) void colsum_kernel(const float* __restrict__ c
 template <typename T>
 __global__ __launch_bounds__(256) void round_rows_kernel(const float* __restrict__ in, T* __restrict__ out, long rows,
                                                          int cols, const int32_t* __restrict__ labels, int classes) {
-  const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 4;
+  const long i = (workgroup() * 256 + threadIdx.x) * 4;
   const long n = rows * cols;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
@@ -335,7 +343,7 @@ __global__ __launch_bounds__(256) void lse_kernel(const float2* __restrict__ sta
                                                   float* __restrict__ lse, float* __restrict__ loss) {
   __shared__ float2 lds[4];
   const int t = threadIdx.x % W;
-  const long row = (long)blockIdx.x * (256 / W) + threadIdx.x / W;
+  const long row = workgroup() * (256 / W) + threadIdx.x / W;
   if (row >= rows) return;  // whole waves (W = 64), or no workgroup at all
   float m = -INFINITY, s = 0.f;
   const float2* p = stats + (size_t)row * nstat;
@@ -601,7 +609,7 @@ static hipError_t pack(int dt, const void* in, void* out, long rows, const void*
                        long ldo, const int32_t* labels, int classes, hipStream_t st) {
   TraceScope ts("pack_kernel", st, (double)(rows + rows2) * (cols + ldo) * dt_size(dt), WORK_BYTE);
   const long chunks = (rows + rows2) * (ldo / (dt == BF16 ? 8 : 4));
-  const dim3 grid((unsigned)((chunks + 255) / 256));
+  const dim3 grid = grid_of((chunks + 255) / 256);
   if (dt == BF16)
     hipLaunchKernelGGL(pack_kernel<bf16_t>, grid, dim3(256), 0, st, (const bf16_t*)in, (bf16_t*)out, rows, (const bf16_t*)in2,
                        (bf16_t*)out2, rows2, cols, ldo, labels, classes);
@@ -653,7 +661,7 @@ hipError_t launch_colsum_rows(const float* dzf, long ld, float* colsum, long row
 hipError_t launch_round_rows(int dt, const float* in, void* out, long rows, int cols, const int32_t* labels, int classes,
                              hipStream_t st) {
   TraceScope ts("round_rows_kernel", st, (double)rows * cols * (4 + dt_size(dt)), WORK_BYTE);
-  const dim3 grid((unsigned)((rows * cols + 1023) / 1024));
+  const dim3 grid = grid_of((rows * cols + 1023) / 1024);
   if (dt == BF16)
     hipLaunchKernelGGL(round_rows_kernel<bf16_t>, grid, dim3(256), 0, st, in, (bf16_t*)out, rows, cols, labels, classes);
   else
@@ -666,7 +674,7 @@ hipError_t launch_lse(const float2* stats, int nstat, const float* zlab, const i
   TraceScope ts("lse_kernel", st, 8.0 * rows * nstat, WORK_BYTE);
   // a wave per row, or, where rows are few, a workgroup per row
   if (rows >= 1024)
-    hipLaunchKernelGGL(lse_kernel<64>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, stats, nstat, zlab, labels, classes,
+    hipLaunchKernelGGL(lse_kernel<64>, grid_of((rows + 3) / 4), dim3(256), 0, st, stats, nstat, zlab, labels, classes,
                        rows, lse, loss);
   else
     hipLaunchKernelGGL(lse_kernel<256>, dim3((unsigned)rows), dim3(256), 0, st, stats, nstat, zlab, labels, classes, rows, lse,

@@ -365,7 +365,8 @@ class Net:
         shape = (self.batch, H, W, C)
         prev = None
         specs = list(workload.layers)
-        fused_loss = fused_loss and len(specs) > 1 and isinstance(specs[-1], wl.SoftmaxCE) and isinstance(specs[-2], wl.FC)
+        if fused_loss and not (len(specs) > 1 and isinstance(specs[-1], wl.SoftmaxCE) and isinstance(specs[-2], wl.FC)):
+            raise ValueError("fused_loss: a fully connected layer and a softmax loss at the end wanted")
         for i, spec in enumerate(specs):
             head = fused_loss and i == len(specs) - 2
             if isinstance(spec, wl.Conv):

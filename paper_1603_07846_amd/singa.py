@@ -671,7 +671,8 @@ _LINEAR_PLANS = {}
 def linear_fwd(x, w, bias=None, act="none", residual=None, keep_z=False, out=None, z=None, workspace=None):
     """Inner product ComputeFeature: y = act(x w^T + bias) + residual, x (..., in), w (out, in), bias fp32.
     keep_z (or z, a tensor for it): also the pre-activation x w^T + bias, which linear_bwd takes; then (y, z) is
-    returned.  act: "none", "relu", "gelu" (erf) or "silu"."""
+    returned.  act: "none", "relu", "gelu" (erf) or "silu".  out may be the residual; no other output of these calls
+    may share memory with an input, but for dx with dx_residual."""
     dtype = x.dtype
     key = (dtype, x.shape, w.shape, act)
     p = _LINEAR_PLANS.get(key)
@@ -806,7 +807,7 @@ def grad_norm(grads, max_norm=float("inf"), stat=None, workspace=None):
 
 
 def clip_grads(grads, max_norm, out=None, stat=None, workspace=None):
-    """grad_norm, then out[i] = scale * grads[i] (in place without out).  Returns (norm, scale) as grad_norm."""
+    """grad_norm, then out[i] = scale * grads[i] (in place without out; no tensor twice).  Returns (norm, scale) as grad_norm."""
     grads = list(grads)
     return _grad_stat(grads, max_norm, grads if out is None else list(out), stat, workspace)
 

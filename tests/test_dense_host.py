@@ -8,6 +8,8 @@ import pytest
 import torch
 
 from paper_1603_07846_amd import singa
+from paper_1603_07846_amd import workloads as wl
+from paper_1603_07846_amd.net import Net
 
 HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "singa_mi_dense.h")
 A = 1 << 20  # an aligned address that nothing is ever read from
@@ -141,3 +143,54 @@ def test_python_checks():
         singa.grad_norm([])
     with pytest.raises(ValueError, match="grads"):
         singa.grad_norm([x])
+
+
+X, W, Y, Z, B2 = (A + i * (1 << 24) for i in range(1, 6))  # far enough apart for every call below
+
+
+@pytest.mark.parametrize("change", [
+    dict(y=X), dict(y=W), dict(z=Y), dict(z=X + 16), dict(y=X + 100 * 64 * 4 - 16), dict(bias=Y + 4), dict(res=Y + 16),
+    dict(z=B2, res=B2)])
+def test_linear_fwd_refuses_shared_memory(change):
+    assert fwd(**{**dict(x=X, w=W, y=Y, z=None, bias=None), **change}) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("change", [
+    dict(dx=X), dict(dx=W), dict(dx=Y), dict(dx=Z), dict(dw=X), dict(dw=A + 16), dict(db=A + 4), dict(res=A + 16),
+    dict(dw=None, db=None, dx=Y)])
+def test_linear_bwd_refuses_shared_memory(change):
+    args = dict(x=X, w=W, dy=Y, z=Z, dx=A, dw=B2, db=A + (1 << 23), ws=A + (1 << 28))
+    assert bwd(**{**args, **change}) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("change", [
+    dict(dx=X), dict(dw=W), dict(db=Z), dict(labels=A), dict(loss=X), dict(dx=Y), dict(dw=X + 100 * 64 * 2 - 16)])
+def test_linear_softmax_ce_refuses_shared_memory(change):
+    args = dict(x=X, w=W, bias=Z, labels=Z + 8192, loss=A, dx=A + 8192, dw=Y, db=B2, ws=A + (1 << 28))
+    assert ce(**{**args, **change}) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("grads,outs,sizes", [
+    ((A, A), (A, A), (10, 10)),                          # a gradient listed twice
+    ((A, A + 16), (A, A + 16), (10, 10)),                # a view of another one
+    ((A, A + 4096), (A + 4096, A), (10, 10)),            # outputs in the other's place
+    ((A, A + 4096), (A + 8192, A + 8208), (10, 10)),     # outputs that overlap
+    ((A, A + 4096), (A + 4, A + 4096), (10, 10)),        # an output a step beside its gradient
+    ((A, A + 64), (A, A + 64), (1000, 1))])
+def test_clipping_refuses_shared_memory(grads, outs, sizes):
+    assert norm(dtypes=(0, 0), grads=grads, outs=outs, sizes=sizes) == UNSUPPORTED
+
+
+def test_sizes_beyond_the_limits_are_refused():
+    # rows x in, rows x out, in x out: 2^37 elements at most
+    for r, i, o in ((1 << 28, 1 << 10, 8), (1 << 28, 8, 1 << 10), (8, 1 << 20, 1 << 18)):
+        assert fwd(rows=r, din=i, dout=o) == UNSUPPORTED
+        assert bwd(rows=r, din=i, dout=o) == UNSUPPORTED
+        assert ce(rows=r, din=i, classes=o) == UNSUPPORTED
+
+
+def test_fused_loss_wants_a_layer_to_fuse():
+    layers = (wl.FC("fc", 6, out_shape=(6, 1, 1)), wl.Relu("relu"), wl.SoftmaxCE())
+    with pytest.raises(ValueError, match="fused_loss"):
+        Net(wl.Workload(51, "a ReLU before the loss", "f32", 2, (4, 6, 6), "normal", layers, classes=6), device="cpu",
+            fused_loss=True)

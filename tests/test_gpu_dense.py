@@ -581,7 +581,6 @@ def test_refusals_on_the_gpu():
     assert e.value.status == -4
 
 
-
 @pytest.mark.parametrize("rows", [3, 150])
 @pytest.mark.parametrize("act", ["gelu", "silu"])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
@@ -600,9 +599,50 @@ def test_activations_far_below_zero(dt, act, rows):
     within("y", y, yr, off + u_of(T) * (yr.abs() + off))
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,din,dout", [(5, 72, 40), (130, 72, 136), (130, 63, 77), (300, 1001, 264)])
+def test_a_row_of_nan_or_infinity_reaches_its_own_outputs_only(rows, din, dout, dt):
+    """The ends of rows, of K and of tiles: what lies beyond them is never multiplied with."""
+    T = DT[dt]
+    g = torch.Generator().manual_seed(31)
+    x, w = rnd(g, rows, din, dtype=T), rnd(g, dout, din, dtype=T)
+    dy = rnd(g, rows, dout, dtype=T)
+    r, c = rows // 2, dout // 2
+    for far in (float("nan"), float("inf")):
+        xx, ww, dd = x.clone(), w.clone(), dy.clone()
+        xx[r] = far
+        bad = ~singa.linear_fwd(xx, w).isfinite()
+        assert bool(bad[r].all()) and int(bad.sum()) == dout
+        ww[c] = far
+        bad = ~singa.linear_fwd(x, ww).isfinite()
+        assert bool(bad[:, c].all()) and int(bad.sum()) == rows
+        dd[r] = far
+        dx, dw, db = singa.linear_bwd(x, w, dd)
+        bad = ~dx.isfinite()
+        assert bool(bad[r].all()) and int(bad.sum()) == din and not bool(dw.isfinite().any()) and not bool(db.isfinite().any())
+        dd = dy.clone()
+        dd[:, c] = far
+        dx, dw, db = singa.linear_bwd(x, w, dd)
+        bad = ~dw.isfinite()
+        assert bool(bad[c].all()) and int(bad.sum()) == din and not bool(dx.isfinite().any()) and int((~db.isfinite()).sum()) == 1
+
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("rows", [1, 8, 24, 64])
 def test_few_rows_of_far_apart_weights(rows, dt):
     """Rows of 16 and 32 KB, where the workgroups begin at different places of K."""
     check_fwd(dt, rows, 8192, 4099, "none", True, False, False)
+
+
+def test_shared_memory_is_refused():
+    g = torch.Generator().manual_seed(32)
+    x, w = rnd(g, 80, 64), rnd(g, 64, 64)
+    with pytest.raises(singa.SingaError):
+        singa.linear_fwd(x, w, out=x)
+    with pytest.raises(singa.SingaError):
+        singa.linear_bwd(x, w, x, dx=x)
+    with pytest.raises(singa.SingaError):
+        singa.clip_grads([w, w], 1.0)
+    with pytest.raises(singa.SingaError):
+        singa.clip_grads([w, w[:3]], 1.0)
+    assert float(singa.grad_norm([w, w])[0]) == pytest.approx(math.sqrt(2) * float(w.double().norm()), rel=4 * F)
