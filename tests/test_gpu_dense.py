@@ -6,7 +6,7 @@ type is one rounding of a stored value, G(n) = (n + 4) 2^-24 the relative
 error of an fp32 sum of n products against the sum of their magnitudes.
   y, z      G(in) S, S = |x| |w|^T + |b|, through an activation whose slope is
             at most 1.13, plus the activation's own error: bf16 results 2^-21
-            of |z| (a polynomial of absolute error 1.5e-7 and the hardware's
+            of |z| (a polynomial of relative error 4.5e-7 and the hardware's
             exponential), fp32 2^-21 as well (a few ulp of erf / exp).
   dz        4 ulp and 2^-20 of |dy| (the slope), rounded to the type: u |dz|,
             or u^3 |dz| where it is kept in three terms (fp32 dw of a smooth
@@ -646,3 +646,45 @@ def test_shared_memory_is_refused():
     with pytest.raises(singa.SingaError):
         singa.clip_grads([w, w[:3]], 1.0)
     assert float(singa.grad_norm([w, w])[0]) == pytest.approx(math.sqrt(2) * float(w.double().norm()), rel=4 * F)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(3, 40, 100), (90, 63, 300), (100, 16, 10007), (1100, 24, 500), (700, 24, 26003)])
+def test_parts_of_the_loss(size, dt):
+    """Each gradient by itself: the same but for the order of sums and, in bf16, one rounding of dz and of the result."""
+    rows, din, classes = size
+    T = DT[dt]
+    g = torch.Generator().manual_seed(33)
+    x, w, b = rnd(g, rows, din, dtype=T), rnd(g, classes, din, dtype=T), rnd(g, classes)
+    labels = dev(torch.randint(-1, classes, (rows,), generator=g, dtype=torch.int32))
+    loss, dx, dw, db = singa.linear_softmax_ce(x, w, labels, b)
+    only = [singa.linear_softmax_ce(x, w, labels, b, need_dw=False), singa.linear_softmax_ce(x, w, labels, b, need_dx=False),
+            singa.linear_softmax_ce(x, w, labels, b, need_dx=False, need_dw=False), singa.linear_softmax_ce(x, w, labels)]
+    bound = 2 * G(max(rows, classes)) + (4 * u_of(T) if T == torch.bfloat16 else 0)
+    for got, want in zip((only[0][1], only[0][3], only[1][2], only[1][3], only[2][3]), (dx, db, dw, db, db)):
+        assert float((got.double() - want.double()).norm() / want.double().norm()) <= bound
+    assert only[0][2] is None and only[1][1] is None and only[2][1] is None and only[3][3] is None
+    for o in only[:3]:
+        assert torch.equal(o[0], loss)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_shapes_of_more_and_fewer_dimensions(dt):
+    T = DT[dt]
+    g = torch.Generator().manual_seed(34)
+    x, w, b = rnd(g, 6, 16, dtype=T), rnd(g, 9, 16, dtype=T), rnd(g, 9)
+    labels = dev(torch.randint(0, 9, (6,), generator=g, dtype=torch.int32))
+    dy = rnd(g, 6, 9, dtype=T)
+    want = singa.linear_fwd(x, w, b), *singa.linear_bwd(x, w, dy), *singa.linear_softmax_ce(x, w, labels, b)
+    x3 = x.view(2, 3, 16)
+    got = (singa.linear_fwd(x3, w, b), *singa.linear_bwd(x3, w, dy.view(2, 3, 9)),
+           *singa.linear_softmax_ce(x3, w, labels.view(2, 3), b))
+    for a, c in zip(want, got):
+        assert torch.equal(a.reshape(-1), c.reshape(-1))
+    assert got[0].shape == (2, 3, 9) and got[1].shape == x3.shape and got[5].shape == x3.shape
+    one = singa.linear_fwd(x[0], w, b), singa.linear_softmax_ce(x[0], w, labels[0], b)
+    assert one[0].shape == (9,) and one[1][0].shape == (2,) and one[1][1].shape == (16,)
+    assert torch.equal(one[0], singa.linear_fwd(x[:1], w, b)[0])
+    none = singa.linear_softmax_ce(x[:0], w, labels[:0], b)
+    assert none[0].tolist() == [0.0] and not bool(none[2].any()) and not bool(none[3].any()) and none[1].shape == (0, 16)
+    assert singa.linear_fwd(x[:0], w, b).shape == (0, 9)
