@@ -100,12 +100,13 @@ hipError_t launch_pair(const Product& dx, const Product& dw, const LossFinish* f
 // them ([M][N rounded up to 8] each, also when it is one) and stops there.
 int product_splits(int dt, int M, int N, int K);
 
-// Whether launch_skinny is the faster one.
-bool product_skinny(int dt, int M, int N, int K);
+// Whether launch_skinny is the faster one (copied: operands for the tiles are
+// needed anyway).
+bool product_skinny(int dt, int M, int N, int K, bool copied);
 // The same product for few rows (M <= SKINNY_ROWS), A and B both K contiguous
-// with ld = K, any alignment: a pass over B.  EPI_OUT and EPI_LSE (STAT_COLS
+// with ld = K, any alignment.  EPI_OUT and EPI_LSE (STAT_COLS
 // of SKINNY_COLS columns).
-constexpr int SKINNY_ROWS = 64, SKINNY_COLS = 16;
+constexpr int SKINNY_ROWS = 512, SKINNY_COLS = 16;
 hipError_t launch_skinny(const Product& p, hipStream_t st);
 
 // Zeros, by a kernel (a captured memset node is not replayed reliably).

@@ -108,7 +108,7 @@ struct FwdWs {
 size_t carve_fwd(int dt, int rows, int in, int out, void* ws, FwdWs* o) {
   Carver c(ws);
   *o = FwdWs{};
-  o->skinny = product_skinny(dt, rows, out, in);
+  o->skinny = product_skinny(dt, rows, out, in, false);
   if (rows == 0 || o->skinny) return 0;
   const size_t es = dt_size(dt);
   o->k = packed(dt, in);
@@ -178,7 +178,7 @@ size_t carve_loss(int dt, int rows, int in, int classes, bool grad, int dw_dt, v
   const size_t es = dt_size(dt);
   o->k = packed(dt, in);
   // (the loss of a few rows alone takes two launches that way, four after tiles)
-  o->skinny = product_skinny(dt, rows, classes, in) || (!grad && rows <= LSE_FINISH_ROWS);
+  o->skinny = product_skinny(dt, rows, classes, in, grad) || (!grad && rows <= LSE_FINISH_ROWS);
   o->ldl = up(classes, 8);
   o->keep = (!o->skinny || grad) && (size_t)rows * o->ldl * 4 <= kKeep;
   o->split = grad && dt == BF16 && dw_dt == F32;

@@ -9,14 +9,15 @@ namespace {
 
 // ------------------------------------------------- product of few rows
 //
-// Reads B (the weights) once, 16 of its rows per workgroup, straight into
-// registers: v_mfma_f32_16x16x32_bf16 (or four v_mfma_f32_16x16x4_f32) takes
+// A workgroup takes 16 rows of B (the weights) and up to 16 MT rows of A,
+// straight into registers: v_mfma_f32_16x16x32_bf16 (or four v_mfma_f32_16x16x4_f32) takes
 // 16 bytes of a row from each lane, 64 consecutive bytes of a row per step, so
 // neither operand needs LDS and any row start will do (ALIGNED: the rows start
 // at 16-byte boundaries; otherwise the same loads without that promise, and the
 // end of a row element by element).  The waves share the K range and add their
-// sums through LDS.  Bound by the bytes of B; U steps (U x 64 bytes of 16
-// rows) are in flight per wave.
+// sums through LDS.  Bound by the bytes of B where A is one block of rows (4096
+// x 32000 bf16, one row: 6.3 TB/s), else by what the caches deliver; U steps (U
+// x 64 bytes of 16 rows) are in flight per wave.
 typedef float f32x4v __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ void mma16(const bf16x8& a, const bf16x8& b, f32x4v& c) {
@@ -57,12 +58,12 @@ __global__ __launch_bounds__(SKINNY_WAVES * 64) void skinny_kernel(const T* __re
   constexpr int VEC = TypeInfo<T>::VEC, U = MT <= 2 ? 8 : 4, STEP = 4 * VEC;
   __shared__ float red[SKINNY_WAVES][MT * 16][16];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, li = lane & 15, kq = lane >> 4;
-  const int n0 = blockIdx.x * 16;
+  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * MT * 16;
   // rows past the end read the last one; their results are not used
   const T* wr = w + (size_t)min(n0 + li, N - 1) * K;
   const T* xr[MT];
 #pragma unroll
-  for (int m = 0; m < MT; ++m) xr[m] = x + (size_t)min(m * 16 + li, M - 1) * K;
+  for (int m = 0; m < MT; ++m) xr[m] = x + (size_t)min(m0 + m * 16 + li, M - 1) * K;
   f32x4v acc[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) acc[m] = f32x4v{0.f, 0.f, 0.f, 0.f};
@@ -104,10 +105,10 @@ __global__ __launch_bounds__(SKINNY_WAVES * 64) void skinny_kernel(const T* __re
   for (int m = 0; m < MT; ++m) *(f32x4v*)&red[wave][m * 16 + li][kq * 4] = acc[m];
   __syncthreads();
   for (int idx = threadIdx.x; idx < MT * 256; idx += SKINNY_WAVES * 64) {
-    const int row = idx >> 4, c = idx & 15, col = n0 + c;
+    const int row = m0 + (idx >> 4), c = idx & 15, col = n0 + c;
     float v = 0.f;
 #pragma unroll
-    for (int s = 0; s < SKINNY_WAVES; ++s) v += red[s][row][c];
+    for (int s = 0; s < SKINNY_WAVES; ++s) v += red[s][idx >> 4][c];
     const bool in = row < M && col < N;
     if (e.bias && in) v += e.bias[col];
     if constexpr (EPI == EPI_OUT) {
@@ -138,12 +139,13 @@ __global__ __launch_bounds__(SKINNY_WAVES * 64) void skinny_kernel(const T* __re
 }
 
 template <typename T, bool ALIGNED, int EPI> hipError_t skinny_rows(const Product& p, hipStream_t st) {
-  const dim3 grid((unsigned)((p.N + 15) / 16)), block(SKINNY_WAVES * 64);
+  const int mt = plan_skinny(p.dt, p.M, p.N, p.K).mt;
+  const dim3 grid((unsigned)((p.N + 15) / 16), (unsigned)((p.M + 16 * mt - 1) / (16 * mt))), block(SKINNY_WAVES * 64);
   const T *x = (const T*)p.a.p, *w = (const T*)p.b.p;
   Epilogue e = p.e;
   if (!e.ldy) e.ldy = p.N;
   TraceScope ts(p.name, st, p.flops, WORK_FLOP);
-  switch ((p.M + 15) / 16) {
+  switch (mt) {
     case 1: hipLaunchKernelGGL((skinny_kernel<T, ALIGNED, 1, EPI>), grid, block, 0, st, x, w, p.M, p.N, p.K, e); break;
     case 2: hipLaunchKernelGGL((skinny_kernel<T, ALIGNED, 2, EPI>), grid, block, 0, st, x, w, p.M, p.N, p.K, e); break;
     default: hipLaunchKernelGGL((skinny_kernel<T, ALIGNED, 4, EPI>), grid, block, 0, st, x, w, p.M, p.N, p.K, e); break;

@@ -16,7 +16,7 @@ size_t pair_partial_bytes(int dt, int Ma, int Na, int Ka, int Mb, int Nb, int Kb
   return pair_pays(dt, p, Ma, Na, Ka, Mb, Nb, Kb) ? partial_bytes_of(p.a, Ma, Na) + partial_bytes_of(p.b, Mb, Nb) : 0;
 }
 
-bool product_skinny(int dt, int M, int N, int K) { return skinny_pays(dt, M, N, K); }
+bool product_skinny(int dt, int M, int N, int K, bool copied) { return skinny_pays(dt, M, N, K, copied); }
 
 int product_splits(int dt, int M, int N, int K) { return plan_product(dt, M, N, K, EPI_OUT).splits; }
 

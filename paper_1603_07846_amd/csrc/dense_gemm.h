@@ -1083,28 +1083,45 @@ inline PairPlan plan_pair(int dt, int Ma, int Na, int Ka, int Mb, int Nb, int Kb
 inline bool pair_pays(int dt, const PairPlan& p, int Ma, int Na, int Ka, int Mb, int Nb, int Kb) {
   return p.t < plan_product(dt, Ma, Na, Ka, EPI_OUT).t + plan_product(dt, Mb, Nb, Kb, EPI_OUT).t + 3;
 }
-// Up to SKINNY_ROWS rows: whether the pass over B without LDS is faster than
-// tiles (and, for odd row lengths, the copies that those need).  Measured, in
-// us, at 1 / 16 / 32 / 64 rows against tiles: bf16 4096 x 4096 6.8 / 9.1 /
-// 12.6 / 20 against 12 .. 15; 50000 x 2048 36 / 47 / 69 / 115 against 33;
-// 1000 x 9216 12 / 18 / 25 / 41 against 13 .. 17; 777 x 1001 5 / 6 / 8 / 12
-// against 16; fp32 4096 x 4096 17 / 20 / 23 / 39 against 26 .. 28.  The model: the
-// runs of steps one wave makes, each slower with more rows, or B's bytes at a
-// rate that longer runs bring nearer to the memory's.
-inline bool skinny_pays(int dt, int M, int N, int K) {
+// Up to SKINNY_ROWS rows: the kernel without LDS (skinny_kernel), in blocks of
+// 16 mt rows, against tiles (and, for odd row lengths, the copies that those
+// need).  Measured, in us, at 16 / 64 / 128 / 256 rows: bf16 1000 x 776 (K x N)
+// 6 / 6 / 5 / 6 against 11; 1001 x 777 6 / 6 / 8 / 13 against 16 .. 17; 4096 x
+// 1000 9 / 9 / 13 / 21 against 13 .. 16; 4096 x 4096 9 / 20 / 38 / 73 against
+// 14 / 15 / 18 / 23; fp32 1001 x 777 5 / 6 / 7 / 10 against 16 .. 20, 4096 x
+// 4096 16 / 39 / 75 / 145 against 26 / 28 / 48 / 83.  A workgroup reads 16 rows
+// of B and its rows of A, 16 bytes of 16 rows per instruction, and both pass
+// through the caches: the time goes with the bytes of a row, and with the
+// workgroups per CU (which do not overlap much where rows are long, hence half
+// of the rounded number).  bf16 rows that start inside a 4-byte word take 2.5 to
+// 3.5 times as long.
+struct SkinnyPlan {
+  int mt;  // blocks of 16 rows per workgroup
+  double t;
+};
+inline SkinnyPlan plan_skinny(int dt, int M, int N, int K) {
+  const double kb = (dt == BF16 ? 2.0 : 4.0) * K / 2048;
+  SkinnyPlan best{1, 1e30};
+  for (int mt = 1; mt <= 4; mt *= 2) {
+    const int r = M < 16 * mt ? M : 16 * mt;
+    const double wgs = (double)(div_up(N, 16) * div_up(M, 16 * mt)) / 256;
+    const double rounds = wgs <= 1 ? 1 : 0.5 * (wgs + (double)(long)(wgs + 0.999));
+    const double odd = dt == BF16 && K % 2 ? 2.4 + 0.07 * (r < 16 ? r : 16) : 1;
+    const double per = odd * kb * (r <= 16 ? 1.37 + 0.03 * r : 1.1 + 0.054 * r), least = 0.25 + 0.15 * mt;
+    const double t = 1.5 + rounds * (per > least ? per : least);
+    if (t < best.t) best = SkinnyPlan{mt, t < 5 ? 5 : t};
+    if (M <= 16 * mt) break;
+  }
+  return best;
+}
+// copied: the tiles' operands are needed for other products as well.
+inline bool skinny_pays(int dt, int M, int N, int K, bool copied) {
   if (M > SKINNY_ROWS) return false;
   const double es = dt == BF16 ? 2 : 4, bytes = es * N * K;
-  const int u = M <= 32 ? 8 : 4, run = 4 * (dt == BF16 ? 32 : 16) * u;
-  const double runs = (double)div_up(K, run);
-  const double per = M <= 16 ? (dt == BF16 ? 0.9 + 0.045 * M : 1.5 + 0.015 * M) : M <= 32 ? 1.2 + 0.04 * M : 0.95 + 0.02 * M;
-  const double rate = 7.4e6 * runs / (runs + 1);
-  const double pass = bytes / rate * (1 + (dt == BF16 ? 0.026 : 0.04) * M);
-  const double odd = dt == BF16 && K % 2 ? 2 : 1;  // rows that start inside a 4-byte word: 16 us for 7.3
-  const double skinny = 4 + odd * (runs * per > pass ? runs * per : pass);
   double tiles = plan_product(dt, M, N, K, EPI_OUT).t;
   if (tiles < 5 + bytes / 5.3e6) tiles = 5 + bytes / 5.3e6;
-  if (K % (dt == BF16 ? 8 : 4)) tiles += 4 + 2 * bytes / 5e6;
-  return skinny < tiles;
+  if (!copied && K % (dt == BF16 ? 8 : 4)) tiles += 4 + 2 * es * ((double)M + N) * K / 5e6;
+  return plan_skinny(dt, M, N, K).t < tiles;
 }
 
 inline size_t partial_bytes_of(const Plan& p, int M, int N) {

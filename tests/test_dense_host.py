@@ -31,8 +31,8 @@ def fwd(dt=0, rows=100, din=64, dout=64, x=A, w=A, bias=A, act=0, res=None, z=No
     (dict(dt=2), UNSUPPORTED), (dict(act=4), UNSUPPORTED), (dict(act=-1), UNSUPPORTED), (dict(rows=-1), SHAPE),
     (dict(din=0), SHAPE), (dict(dout=0), SHAPE), (dict(din=(1 << 20) + 1), UNSUPPORTED), (dict(x=None), NULL),
     (dict(w=None), NULL), (dict(y=None), NULL), (dict(x=A + 4), ALIGN), (dict(y=A + 8), ALIGN), (dict(z=A + 2), ALIGN),
-    (dict(res=A + 4), ALIGN), (dict(bias=A + 2), ALIGN), (dict(din=63, nbytes=100), WORKSPACE),
-    (dict(din=63, ws=None), WORKSPACE), (dict(din=63, ws=A + 4), ALIGN), (dict(rows=1 << 29), UNSUPPORTED),
+    (dict(res=A + 4), ALIGN), (dict(bias=A + 2), ALIGN), (dict(rows=1000, din=63, nbytes=100), WORKSPACE),
+    (dict(rows=1000, din=63, ws=None), WORKSPACE), (dict(rows=1000, din=63, ws=A + 4), ALIGN), (dict(rows=1 << 29), UNSUPPORTED),
     (dict(rows=0, x=None, y=None), 0)])
 def test_linear_fwd_refuses(change, want):
     assert fwd(**change) == want
