@@ -93,9 +93,11 @@ hipError_t launch_product(const Product& p, float* partial, hipStream_t st);
 // contiguous) and weight gradient (both rows contiguous), in one launch where
 // that is faster; workspace: the larger of the two products' and this.
 size_t pair_partial_bytes(int dt, int Ma, int Na, int Ka, int Mb, int Nb, int Kb);
-// finish (may be null): done by further workgroups of that launch, or before.
+// sums, finish (may be null): done by further workgroups of that launch, or before.
+struct ColumnSums;
 struct LossFinish;
-hipError_t launch_pair(const Product& dx, const Product& dw, const LossFinish* finish, float* partial, hipStream_t st);
+hipError_t launch_pair(const Product& dx, const Product& dw, const ColumnSums* sums, const LossFinish* finish, float* partial,
+                       hipStream_t st);
 // Number of partial sums of that product; launch_product with `raw` writes
 // them ([M][N rounded up to 8] each, also when it is one) and stops there.
 int product_splits(int dt, int M, int N, int K);
@@ -123,9 +125,20 @@ hipError_t launch_pack2(int dt, const void* in, void* out, long rows, const void
 // (may be null) the sums of the unrounded dz; dz may be null.
 hipError_t launch_dact(int dt, int act, const void* dy, const void* z, void* dz, void* more, float* colsum, long rows,
                        long rows_padded, int cols, long ldz, hipStream_t st);
-// out[c] (+)= alpha (null: 1) times the sum of colsum[0 .. groups - 1][c] (in order)
-hipError_t launch_colsum(const float* colsum, float* out, long groups, int cols, int add, const float* alpha,
-                         hipStream_t st);
+// out[c] (+)= alpha (null: 1) times the sum of src[0 .. rows - 1][c], in a fixed
+// order; SUM_COLS columns per workgroup of 256 threads
+constexpr int SUM_COLS = 16;
+struct ColumnSums {
+  const void* src;  // [rows][cols] of type dt
+  int dt;
+  long rows;
+  int cols;
+  float* out;
+  int add;
+  const float* alpha;
+};
+inline unsigned sums_wgs(const ColumnSums& s) { return (unsigned)((s.cols + SUM_COLS - 1) / SUM_COLS); }
+hipError_t launch_column_sums(const ColumnSums& s, hipStream_t st);
 // out (T [rows][cols]) = in (fp32 [rows][cols]), zero in rows without a valid label
 hipError_t launch_round_rows(int dt, const float* in, void* out, long rows, int cols, const int32_t* labels,
                              int classes, hipStream_t st);

@@ -225,9 +225,11 @@ size_t carve_loss(int dt, int rows, int in, int classes, bool grad, int dw_dt, v
 
 Operand op(const void* p, long ld, bool kc) { return Operand{p, ld, kc}; }
 
-hipError_t launch_gradients(const Product* dx, const Product* dw, const LossFinish* finish, float* partial, hipStream_t st) {
-  if (dx && dw) return launch_pair(*dx, *dw, finish, partial, st);
-  const hipError_t e = finish ? launch_loss_finish(*finish, st) : hipSuccess;
+hipError_t launch_gradients(const Product* dx, const Product* dw, const ColumnSums* sums, const LossFinish* finish,
+                            float* partial, hipStream_t st) {
+  if (dx && dw) return launch_pair(*dx, *dw, sums, finish, partial, st);
+  hipError_t e = sums ? launch_column_sums(*sums, st) : hipSuccess;
+  if (e == hipSuccess && finish) e = launch_loss_finish(*finish, st);
   return e == hipSuccess && (dx || dw) ? launch_product(dx ? *dx : *dw, partial, st) : e;
 }
 
@@ -337,11 +339,13 @@ int singa_linear_bwd(singa_dtype dtype, int rows, int in, int out, const void* x
   BwdWs o;
   carve_bwd(dtype, rows, in, out, act, dw_dtype, ws, &o);
   const bool split = o.split && dw;
-  if (o.own_dz || db)
+  // few rows of a dy that goes into the products as it is: db straight from it
+  const bool direct = !o.own_dz && rows <= FINISH_ROWS;
+  if (o.own_dz || (db && !direct))
     e = launch_dact(dtype, act, dy, z, o.own_dz ? o.dz : nullptr, split ? o.more : nullptr, db ? o.colsum : nullptr, rows,
                     o.rows_padded, out, o.ldz, st);
-  if (e == hipSuccess && db)
-    e = launch_colsum(o.colsum, db, up(rows, COLSUM_ROWS) / COLSUM_ROWS, out, accumulate, nullptr, st);
+  const ColumnSums sums = direct ? ColumnSums{dy, dtype, rows, out, db, accumulate, nullptr}
+                                 : ColumnSums{o.colsum, F32, up(rows, COLSUM_ROWS) / COLSUM_ROWS, out, db, accumulate, nullptr};
   const void* dz = o.own_dz ? o.dz : dy;
   if (o.k.copy && (dx || dw) && e == hipSuccess) {
     e = launch_pack2(dtype, x, o.xp, dw ? rows : 0, w, o.wp, dx ? out : 0, in, o.k.ld, st);
@@ -374,7 +378,7 @@ int singa_linear_bwd(singa_dtype dtype, int rows, int in, int out, const void* x
     q.e.out_f32 = dw_dtype == SINGA_F32;
     q.e.add = accumulate != 0;
   }
-  if (e == hipSuccess) e = launch_gradients(dx ? &p : nullptr, dw ? &q : nullptr, nullptr, o.partial, st);
+  if (e == hipSuccess) e = launch_gradients(dx ? &p : nullptr, dw ? &q : nullptr, db ? &sums : nullptr, nullptr, o.partial, st);
   return status(e);
 }
 
@@ -531,7 +535,7 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
     } else if (db && !finish) {
       e = launch_colsum_rows(o.logits, o.ldl, o.colsum, rows, classes, labels, classes, st);
     }
-    if (e == hipSuccess && db && !finish) e = launch_colsum(o.colsum, db + c0, groups, n, accumulate, o.unit, st);
+    const ColumnSums sums{o.colsum, F32, groups, n, db ? db + c0 : nullptr, accumulate, o.unit};
     Product q, v;
     if (dx) {
       q.name = "product_kernel<bwd_data>";
@@ -567,7 +571,9 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
       v.e.out_f32 = dw_dtype == SINGA_F32;
       v.e.add = accumulate != 0;
     }
-    if (e == hipSuccess) e = launch_gradients(dx ? &q : nullptr, dw ? &v : nullptr, finish ? &fin : nullptr, o.partial, st);
+    if (e == hipSuccess)
+      e = launch_gradients(dx ? &q : nullptr, dw ? &v : nullptr, db && !finish ? &sums : nullptr, finish ? &fin : nullptr,
+                           o.partial, st);
   }
   if (e == hipSuccess && dx && !o.one) e = launch_round_rows(dtype, o.dxf, dx, rows, in, labels, classes, st);
   return status(e);

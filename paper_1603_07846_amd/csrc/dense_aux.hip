@@ -284,22 +284,9 @@ __global__ __launch_bounds__(256) void colsum_rows_kernel(const float* __restric
   if (tr == 0 && col < cols) colsum[(long)blockIdx.x * cols + col] = red[0][tc] + red[1][tc] + red[2][tc] + red[3][tc];
 }
 
-// 32 columns per workgroup, eight threads per column.
-__global__ __launch_bounds__(256) void colsum_kernel(const float* __restrict__ colsum, float* __restrict__ out, long groups,
-                                                     int cols, int add, const float* __restrict__ alpha) {
-  __shared__ float red[8][32];
-  const int tc = threadIdx.x & 31, tr = threadIdx.x >> 5, col = blockIdx.x * 32 + tc;
-  float s = 0.f;
-  if (col < cols)
-    for (long g = tr; g < groups; g += 8) s += colsum[g * cols + col];
-  red[tr][tc] = s;
-  __syncthreads();
-  if (tr || col >= cols) return;
-  s = 0.f;
-#pragma unroll
-  for (int r = 0; r < 8; ++r) s += red[r][tc];
-  if (alpha) s *= alpha[0];
-  out[col] = add ? out[col] + s : s;
+__global__ __launch_bounds__(256) void column_sums_kernel(ColumnSums a) {
+  __shared__ __align__(16) char lds[SUMS_LDS];
+  column_sums(a, blockIdx.x, lds);
 }
 
 template <typename T>
@@ -645,10 +632,9 @@ hipError_t launch_dact(int dt, int act, const void* dy, const void* z, void* dz,
   return hipGetLastError();
 }
 
-hipError_t launch_colsum(const float* colsum, float* out, long groups, int cols, int add, const float* alpha, hipStream_t st) {
-  TraceScope ts("colsum_kernel", st, 4.0 * groups * cols, WORK_BYTE);
-  hipLaunchKernelGGL(colsum_kernel, dim3((unsigned)((cols + 31) / 32)), dim3(256), 0, st, colsum, out, groups, cols, add,
-                     alpha);
+hipError_t launch_column_sums(const ColumnSums& s, hipStream_t st) {
+  TraceScope ts("column_sums_kernel", st, (double)dt_size(s.dt) * s.rows * s.cols, WORK_BYTE);
+  hipLaunchKernelGGL(column_sums_kernel, dim3(sums_wgs(s)), dim3(256), 0, st, s);
   return hipGetLastError();
 }
 

@@ -5,7 +5,8 @@
 namespace singa {
 
 hipError_t launch_product_bf16(const Product& p, float* partial, hipStream_t st);
-hipError_t launch_pair_bf16(const Product& dx, const Product& dw, const LossFinish* finish, float* partial, hipStream_t st);
+hipError_t launch_pair_bf16(const Product& dx, const Product& dw, const ColumnSums* sums, const LossFinish* finish,
+                            float* partial, hipStream_t st);
 
 size_t product_partial_bytes(int dt, int M, int N, int K, int epi) {
   return partial_bytes_of(plan_product(dt, M, N, K, epi), M, N);
@@ -24,8 +25,10 @@ hipError_t launch_product(const Product& p, float* partial, hipStream_t st) {
   return p.dt == BF16 ? launch_product_bf16(p, partial, st) : launch_product_t<float>(p, partial, st);
 }
 
-hipError_t launch_pair(const Product& dx, const Product& dw, const LossFinish* finish, float* partial, hipStream_t st) {
-  return dx.dt == BF16 ? launch_pair_bf16(dx, dw, finish, partial, st) : launch_pair_t<float>(dx, dw, finish, partial, st);
+hipError_t launch_pair(const Product& dx, const Product& dw, const ColumnSums* sums, const LossFinish* finish, float* partial,
+                       hipStream_t st) {
+  return dx.dt == BF16 ? launch_pair_bf16(dx, dw, sums, finish, partial, st)
+                       : launch_pair_t<float>(dx, dw, sums, finish, partial, st);
 }
 
 }  // namespace singa

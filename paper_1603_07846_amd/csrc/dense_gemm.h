@@ -422,6 +422,31 @@ __device__ __forceinline__ double block_sum(double v, double* lds) {
   return s;
 }
 
+// Sums of SUM_COLS columns, 16 threads each (ColumnSums).
+constexpr int SUMS_LDS = 16 * (SUM_COLS + 1) * 4;
+template <typename T> __device__ __forceinline__ float column_part(const T* p, long rows, int cols, int tr) {
+  float s = 0.f;
+#pragma unroll 8
+  for (long r = tr; r < rows; r += 256 / SUM_COLS) s += elem_f(p[r * cols]);
+  return s;
+}
+__device__ __forceinline__ void column_sums(const ColumnSums& a, int wg, char* smem) {
+  float* const red = (float*)smem;
+  const int tc = threadIdx.x % SUM_COLS, tr = threadIdx.x / SUM_COLS, col = wg * SUM_COLS + tc;
+  float s = 0.f;
+  if (col < a.cols)
+    s = a.dt == BF16 ? column_part((const bf16_t*)a.src + col, a.rows, a.cols, tr)
+                     : column_part((const float*)a.src + col, a.rows, a.cols, tr);
+  red[tr * (SUM_COLS + 1) + tc] = s;
+  __syncthreads();
+  if (tr || col >= a.cols) return;
+  s = 0.f;
+#pragma unroll
+  for (int r = 0; r < 256 / SUM_COLS; ++r) s += red[r * (SUM_COLS + 1) + tc];
+  if (a.alpha) s *= a.alpha[0];
+  a.out[col] = a.add ? a.out[col] + s : s;
+}
+
 // For up to FINISH_ROWS rows: the mean, and the bias gradient from the
 // unrounded dlogits, FINISH_COLS columns per workgroup of 256 threads.  Each
 // workgroup counts the rows for itself; the first one writes the mean.
@@ -942,10 +967,12 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : FM == 2 ? 2 : 4) void pr
 
 // The two products of a layer's gradients in one launch, source gradient
 // first: neither leaves the chip half empty while the other waits.
-// What is left of a loss (LossFinish) rides along in further workgroups.
+// What is left of the bias gradient (ColumnSums: 5 us by itself) or of a loss
+// (LossFinish) rides along in further workgroups.
 struct PairArgs {
   GemmArgs dx, dw;
-  int wgs_dx, wgs;
+  int wgs_dx, wgs, wgs_sums;  // workgroups: of dx, of both products, and with the sums'
+  ColumnSums sums;
   LossFinish finish;
 };
 template <typename T, int FM, int FN>
@@ -956,8 +983,10 @@ __global__ __launch_bounds__(256, FM == 4 ? 1 : FM == 2 ? 2 : 4) void product_pa
     product_tile<T, true, false, 2, 2, FM, FN, EPI_OUT>(p.dx, blockIdx.x, smem);
   else if ((int)blockIdx.x < p.wgs)
     product_tile<T, false, false, 2, 2, FM, FN, EPI_OUT>(p.dw, (int)blockIdx.x - p.wgs_dx, smem);
+  else if ((int)blockIdx.x < p.wgs_sums)
+    column_sums(p.sums, (int)blockIdx.x - p.wgs, smem);
   else
-    loss_finish(p.finish, (int)blockIdx.x - p.wgs, smem);
+    loss_finish(p.finish, (int)blockIdx.x - p.wgs_sums, smem);
 }
 
 // Adds the partial sums of a split product in order and finishes them.
@@ -1197,10 +1226,12 @@ template <typename T> hipError_t launch_product_t(const Product& p, float* parti
 }
 
 template <typename T>
-hipError_t launch_pair_t(const Product& dx, const Product& dw, const LossFinish* finish, float* partial, hipStream_t st) {
+hipError_t launch_pair_t(const Product& dx, const Product& dw, const ColumnSums* sums, const LossFinish* finish,
+                         float* partial, hipStream_t st) {
   const PairPlan pl = plan_pair(dx.dt, dx.M, dx.N, dx.K, dw.M, dw.N, dw.K);
   if (!pair_pays(dx.dt, pl, dx.M, dx.N, dx.K, dw.M, dw.N, dw.K)) {
-    hipError_t e = finish ? launch_loss_finish(*finish, st) : hipSuccess;
+    hipError_t e = sums ? launch_column_sums(*sums, st) : hipSuccess;
+    if (e == hipSuccess && finish) e = launch_loss_finish(*finish, st);
     if (e == hipSuccess) e = launch_product_t<T>(dx, partial, st);
     return e == hipSuccess ? launch_product_t<T>(dw, partial, st) : e;
   }
@@ -1209,8 +1240,10 @@ hipError_t launch_pair_t(const Product& dx, const Product& dw, const LossFinish*
   a.dw = args_of<T>(dw, pl.b, partial + partial_bytes_of(pl.a, dx.M, dx.N) / 4);
   a.wgs_dx = (int)wgs_of(a.dx);
   a.wgs = (int)(wgs_of(a.dx) + wgs_of(a.dw));
+  a.wgs_sums = a.wgs + (sums ? (int)sums_wgs(*sums) : 0);
+  if (sums) a.sums = *sums;
   if (finish) a.finish = *finish;
-  const dim3 grid((unsigned)a.wgs + (finish ? finish_wgs(*finish) : 0u));
+  const dim3 grid((unsigned)a.wgs_sums + (finish ? finish_wgs(*finish) : 0u));
   {
     TraceScope ts("product_pair_kernel", st, dx.flops + dw.flops, WORK_FLOP);
     constexpr bool F = sizeof(T) == 4;
