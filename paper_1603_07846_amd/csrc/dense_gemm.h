@@ -971,7 +971,7 @@ __global__ __launch_bounds__(WM* WN * 64, FM == 4 ? 1 : FM == 2 ? 2 : 4) void pr
 // (LossFinish) rides along in further workgroups.
 struct PairArgs {
   GemmArgs dx, dw;
-  int wgs_sums, sums_at, wgs_dx, wgs;  // workgroups: of the sums, the first of those; of dx, of both products
+  int wgs_dx, wgs, wgs_sums;  // workgroups: of dx, of both products, and with the sums'
   ColumnSums sums;
   LossFinish finish;
 };
@@ -979,12 +979,14 @@ template <typename T, int FM, int FN>
 __global__ __launch_bounds__(256, FM == 4 ? 1 : FM == 2 ? 2 : 4) void product_pair_kernel(PairArgs p) {
   constexpr int S1 = Shape<T, true, false, 2, 2, FM, FN>::SMEM, S2 = Shape<T, false, false, 2, 2, FM, FN>::SMEM;
   __shared__ __align__(1024) char smem[S1 > S2 ? S1 : S2];
-  int wg = blockIdx.x;
-  if (wg >= p.sums_at && wg < p.sums_at + p.wgs_sums) return column_sums(p.sums, wg - p.sums_at, smem);
-  if (wg >= p.sums_at) wg -= p.wgs_sums;
-  if (wg < p.wgs_dx) return product_tile<T, true, false, 2, 2, FM, FN, EPI_OUT>(p.dx, wg, smem);
-  if (wg < p.wgs) return product_tile<T, false, false, 2, 2, FM, FN, EPI_OUT>(p.dw, wg - p.wgs_dx, smem);
-  loss_finish(p.finish, wg - p.wgs, smem);
+  if ((int)blockIdx.x < p.wgs_dx)
+    product_tile<T, true, false, 2, 2, FM, FN, EPI_OUT>(p.dx, blockIdx.x, smem);
+  else if ((int)blockIdx.x < p.wgs)
+    product_tile<T, false, false, 2, 2, FM, FN, EPI_OUT>(p.dw, (int)blockIdx.x - p.wgs_dx, smem);
+  else if ((int)blockIdx.x < p.wgs_sums)
+    column_sums(p.sums, (int)blockIdx.x - p.wgs, smem);
+  else
+    loss_finish(p.finish, (int)blockIdx.x - p.wgs_sums, smem);
 }
 
 // Adds the partial sums of a split product in order and finishes them.
@@ -1238,14 +1240,10 @@ hipError_t launch_pair_t(const Product& dx, const Product& dw, const ColumnSums*
   a.dw = args_of<T>(dw, pl.b, partial + partial_bytes_of(pl.a, dx.M, dx.N) / 4);
   a.wgs_dx = (int)wgs_of(a.dx);
   a.wgs = (int)(wgs_of(a.dx) + wgs_of(a.dw));
-  a.wgs_sums = sums ? (int)sums_wgs(*sums) : 0;
+  a.wgs_sums = a.wgs + (sums ? (int)sums_wgs(*sums) : 0);
   if (sums) a.sums = *sums;
-  // First, so that they are not the launch's tail (256 x 9216 x 4096 bf16: 76 ->
-  // 71 us, small calls 1 us), unless they are so many that tiles would pile up on
-  // the CUs that are through with them (fp32 435 x 3160 x 13688: 653 -> 805 us).
-  a.sums_at = a.wgs_sums <= 256 ? 0 : a.wgs;
   if (finish) a.finish = *finish;
-  const dim3 grid((unsigned)(a.wgs_sums + a.wgs) + (finish ? finish_wgs(*finish) : 0u));
+  const dim3 grid((unsigned)a.wgs_sums + (finish ? finish_wgs(*finish) : 0u));
   {
     TraceScope ts("product_pair_kernel", st, dx.flops + dw.flops, WORK_FLOP);
     constexpr bool F = sizeof(T) == 4;
