@@ -121,8 +121,9 @@ hipError_t launch_pack(int dt, const void* in, void* out, long rows, int cols, l
 hipError_t launch_pack2(int dt, const void* in, void* out, long rows, const void* in2, void* out2, long rows2, int cols,
                         long ldo, hipStream_t st);
 // dz = dy act'(z) as T [rows_padded][ldz] (zero past rows and cols), more (may
-// be null) its further terms, colsum [ceil(rows / COLSUM_ROWS)][cols]
-// (may be null) the sums of the unrounded dz; dz may be null.
+// be null) its further terms, colsum [ceil(rows / dact_rows())][cols] (may be
+// null) the sums of the unrounded dz; dz may be null.
+int dact_rows(long rows, int cols);  // rows per workgroup
 hipError_t launch_dact(int dt, int act, const void* dy, const void* z, void* dz, void* more, float* colsum, long rows,
                        long rows_padded, int cols, long ldz, hipStream_t st);
 // out[c] (+)= alpha (null: 1) times the sum of src[0 .. rows - 1][c], in a fixed

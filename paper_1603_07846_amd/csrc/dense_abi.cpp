@@ -128,7 +128,7 @@ size_t gradient_partial_bytes(int dt, int rows, int in, int out, int kw) {
 
 struct BwdWs {
   Packed k;
-  long ldz, rows_padded;
+  long ldz, rows_padded, groups;
   bool own_dz, split;  // dz in the workspace; in TERMS terms
   void *dz, *more, *xp, *wp;
   float *colsum, *partial;
@@ -150,7 +150,8 @@ size_t carve_bwd(int dt, int rows, int in, int out, int act, int dw_dt, void* ws
   o->more = o->split ? (char*)o->dz + half * es : nullptr;
   o->xp = c.take(o->k.copy ? (size_t)rows * o->k.ld * es : 0);
   o->wp = c.take(o->k.copy ? (size_t)out * o->k.ld * es : 0);
-  o->colsum = c.take<float>(up(rows, COLSUM_ROWS) / COLSUM_ROWS * (size_t)out);
+  o->groups = (rows + dact_rows(rows, out) - 1L) / dact_rows(rows, out);
+  o->colsum = c.take<float>(o->groups * (size_t)out);
   const int kw = (int)(o->rows_padded * (o->split ? TERMS : 1));
   o->partial = (float*)c.take(gradient_partial_bytes(dt, rows, in, out, kw));
   return c.bytes();
@@ -345,7 +346,7 @@ int singa_linear_bwd(singa_dtype dtype, int rows, int in, int out, const void* x
     e = launch_dact(dtype, act, dy, z, o.own_dz ? o.dz : nullptr, split ? o.more : nullptr, db ? o.colsum : nullptr, rows,
                     o.rows_padded, out, o.ldz, st);
   const ColumnSums sums = direct ? ColumnSums{dy, dtype, rows, out, db, accumulate, nullptr}
-                                 : ColumnSums{o.colsum, F32, up(rows, COLSUM_ROWS) / COLSUM_ROWS, out, db, accumulate, nullptr};
+                                 : ColumnSums{o.colsum, F32, o.groups, out, db, accumulate, nullptr};
   const void* dz = o.own_dz ? o.dz : dy;
   if (o.k.copy && (dx || dw) && e == hipSuccess) {
     e = launch_pack2(dtype, x, o.xp, dw ? rows : 0, w, o.wp, dx ? out : 0, in, o.k.ld, st);

@@ -203,24 +203,25 @@ __global__ __launch_bounds__(256) void zero_kernel(uint16_t* p, size_t n) {
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = 0;
 }
 
-// A workgroup: COLSUM_ROWS rows of 256 columns, a thread 8 columns of every
-// eighth row.
+// A workgroup: `rpw` rows of 256 columns, a thread 8 columns of every eighth row.
+// Bound by memory (4000 x 4096 bf16: 4.0 TB/s), few rows by the latency of a
+// thread's rows one after the other, so that a workgroup takes fewer of them.
 template <typename T>
 __global__ __launch_bounds__(256) void dact_kernel(int act, const T* __restrict__ dy, const T* __restrict__ z,
                                                    T* __restrict__ dz, bf16_t* __restrict__ more, float* __restrict__ colsum,
-                                                   long rows, long rows_padded, int cols, long ldz) {
-  __shared__ float red[8][256];
+                                                   long rows, long rows_padded, int cols, long ldz, int rpw) {
+  __shared__ float red[8][8 * 33];  // column 8 c + j at 33 j + c: no two lanes of a write in one bank
   const int tc = threadIdx.x & 31, tr = threadIdx.x >> 5;
   const int col = blockIdx.y * 256 + tc * 8;
-  const long row0 = (long)blockIdx.x * COLSUM_ROWS;
+  const long row0 = (long)blockIdx.x * rpw;
   const bool vec = cols % 8 == 0;
   float cs[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) cs[j] = 0.f;
   if (col < ldz) {
 #pragma unroll 2
-    for (int i = 0; i < COLSUM_ROWS / 8; ++i) {
-      const long row = row0 + i * 8 + tr;
+    for (int i = 0; i < rpw; i += 8) {
+      const long row = row0 + i + tr;
       if (row >= rows_padded) break;
       float v[8], u[8];
 #pragma unroll
@@ -258,13 +259,13 @@ __global__ __launch_bounds__(256) void dact_kernel(int act, const T* __restrict_
   }
   if (!colsum) return;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) red[tr][tc * 8 + j] = cs[j];
+  for (int j = 0; j < 8; ++j) red[tr][j * 33 + tc] = cs[j];
   __syncthreads();
   const int c = blockIdx.y * 256 + threadIdx.x;
   if (c >= cols || row0 >= rows) return;
   float s = 0.f;
 #pragma unroll
-  for (int r = 0; r < 8; ++r) s += red[r][threadIdx.x];
+  for (int r = 0; r < 8; ++r) s += red[r][(threadIdx.x & 7) * 33 + (threadIdx.x >> 3)];
   colsum[(long)blockIdx.x * cols + c] = s;
 }
 
@@ -618,17 +619,26 @@ hipError_t launch_pack2(int dt, const void* in, void* out, long rows, const void
   return pack(dt, in, out, rows, in2, out2, rows2, cols, ldo, nullptr, 0, st);
 }
 
+// Halved until there are two workgroups per CU (256 x 4096 bf16, GELU: 64
+// workgroups of 64 rows took 9.6 us).
+int dact_rows(long rows, int cols) {
+  int rpw = COLSUM_ROWS;
+  while (rpw > 8 && (rows + rpw - 1) / rpw * ((cols + 255) / 256) < 512) rpw /= 2;
+  return rpw;
+}
+
 hipError_t launch_dact(int dt, int act, const void* dy, const void* z, void* dz, void* more, float* colsum, long rows,
                        long rows_padded, int cols, long ldz, hipStream_t st) {
-  const dim3 grid((unsigned)((rows_padded + COLSUM_ROWS - 1) / COLSUM_ROWS), (unsigned)((ldz + 255) / 256));
+  const int rpw = dact_rows(rows, cols);
+  const dim3 grid((unsigned)((rows_padded + rpw - 1) / rpw), (unsigned)((ldz + 255) / 256));
   TraceScope ts("dact_kernel", st, (double)rows * cols * dt_size(dt) * (1 + (act != 0) + (dz != nullptr) + (more ? TERMS - 1 : 0)),
                 WORK_BYTE);
   if (dt == BF16)
     hipLaunchKernelGGL(dact_kernel<bf16_t>, grid, dim3(256), 0, st, act, (const bf16_t*)dy, (const bf16_t*)z, (bf16_t*)dz,
-                       (bf16_t*)more, colsum, rows, rows_padded, cols, ldz);
+                       (bf16_t*)more, colsum, rows, rows_padded, cols, ldz, rpw);
   else
     hipLaunchKernelGGL(dact_kernel<float>, grid, dim3(256), 0, st, act, (const float*)dy, (const float*)z, (float*)dz,
-                       (bf16_t*)nullptr, colsum, rows, rows_padded, cols, ldz);
+                       (bf16_t*)nullptr, colsum, rows, rows_padded, cols, ldz, rpw);
   return hipGetLastError();
 }
 

@@ -688,3 +688,18 @@ def test_shapes_of_more_and_fewer_dimensions(dt):
     none = singa.linear_softmax_ce(x[:0], w, labels[:0], b)
     assert none[0].tolist() == [0.0] and not bool(none[2].any()) and not bool(none[3].any()) and none[1].shape == (0, 16)
     assert singa.linear_fwd(x[:0], w, b).shape == (0, 9)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(100, 1001, 777), (400, 63, 256), (512, 512, 500), (201, 130, 33), (65, 2000, 48)])
+def test_several_blocks_of_few_rows(size, dt):
+    check_fwd(dt, *size, "silu", True, True, True)
+    check_ce(dt, size[0], size[1], size[2], grad=False, padded=0.2)
+    check_ce(dt, size[0], size[1], size[2], padded=0.2)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(911, 40, 106), (70, 16, 1000), (17, 24, 5000), (3000, 16, 2056)])
+def test_bias_gradients_of_few_and_many_rows(size, dt):
+    check_bwd(dt, *size, "gelu")
+    check_bwd(dt, *size, "none", accumulate=True)
