@@ -149,8 +149,13 @@ hipError_t launch_lse(const float2* stats, int nstat, const float* zlab, const i
 // loss[0] = mean of loss[1 ..] over the counted rows, unit = scale / count (0 when none; may be null)
 hipError_t launch_loss_mean(const int32_t* labels, int classes, long rows, float* loss, float* unit, float scale,
                             hipStream_t st);
-// The same two at once, for few rows (a workgroup goes through them).
+// The same two at once, for few rows: one workgroup goes through them, row by
+// row (LSE_FINISH_ROWS of any length) or a wave per row, eight rounds at most
+// (a launch less: 13 x 64 x 7817 18 -> 15 us).
 constexpr int LSE_FINISH_ROWS = 4;
+inline bool lse_finish_pays(int rows, int nstat) {
+  return rows <= LSE_FINISH_ROWS || (long)((rows + 15) / 16) * ((nstat + 63) / 64) <= 8;
+}
 hipError_t launch_lse_finish(const float2* stats, int nstat, const float* zlab, const int32_t* labels, int classes, int rows,
                              float* loss, hipStream_t st);
 // Rows of kept logits: z holds `splits` partial sums [rows][ldz] of them (the

@@ -502,7 +502,7 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
       p.name = o.skinny ? "skinny_kernel" : "product_kernel<lse>";
       e = o.skinny ? launch_skinny(p, st) : launch_product(p, nullptr, st);
     }
-    if (!grad && rows <= LSE_FINISH_ROWS)
+    if (!grad && lse_finish_pays(rows, o.nstat))
       return status(e == hipSuccess ? launch_lse_finish(o.stats, o.nstat, o.zlab, labels, classes, rows, loss, st) : e);
     if (e == hipSuccess) e = launch_lse(o.stats, o.nstat, o.zlab, labels, classes, rows, o.lse, loss, st);
   }

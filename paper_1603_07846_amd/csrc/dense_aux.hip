@@ -584,6 +584,33 @@ __global__ __launch_bounds__(1024) void lse_finish_kernel(const float2* __restri
   if (threadIdx.x == 0) loss[0] = n ? (float)(sum / n) : 0.f;
 }
 
+// The same, a wave per row: few rows of few column groups.
+__global__ __launch_bounds__(1024) void lse_finish_rows_kernel(const float2* __restrict__ stats, int nstat,
+                                                               const float* __restrict__ zlab,
+                                                               const int32_t* __restrict__ labels, int classes, int rows,
+                                                               float* __restrict__ loss) {
+  __shared__ double lds[16];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  double sum = 0, n = 0;
+  for (int row = wave; row < rows; row += 16) {
+    float m = -INFINITY, s = 0.f;
+    for (int i = lane; i < nstat; i += 64) {
+      const float2 p = stats[(size_t)row * nstat + i];
+      merge(m, s, p.x, p.y);
+    }
+    merge_all<64>(m, s, nullptr);
+    if (lane) continue;
+    const bool ok = label_ok(labels[row], classes);
+    const float l = ok ? m + logf(s) - zlab[row] : 0.f;
+    loss[1 + row] = l;
+    sum += l;
+    n += ok;
+  }
+  n = block_sum(n, lds);
+  sum = block_sum(sum, lds);
+  if (threadIdx.x == 0) loss[0] = n > 0 ? (float)(sum / n) : 0.f;
+}
+
 }  // namespace
 
 hipError_t launch_zero(void* p, size_t bytes, hipStream_t st) {
@@ -736,7 +763,10 @@ hipError_t launch_loss_finish(const LossFinish& f, hipStream_t st) {
 hipError_t launch_lse_finish(const float2* stats, int nstat, const float* zlab, const int32_t* labels, int classes, int rows,
                              float* loss, hipStream_t st) {
   TraceScope ts("lse_finish_kernel", st, 8.0 * rows * nstat, WORK_BYTE);
-  hipLaunchKernelGGL(lse_finish_kernel, dim3(1), dim3(1024), 0, st, stats, nstat, zlab, labels, classes, rows, loss);
+  if (rows <= LSE_FINISH_ROWS)
+    hipLaunchKernelGGL(lse_finish_kernel, dim3(1), dim3(1024), 0, st, stats, nstat, zlab, labels, classes, rows, loss);
+  else
+    hipLaunchKernelGGL(lse_finish_rows_kernel, dim3(1), dim3(1024), 0, st, stats, nstat, zlab, labels, classes, rows, loss);
   return hipGetLastError();
 }
 
