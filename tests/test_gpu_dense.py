@@ -703,3 +703,39 @@ def test_several_blocks_of_few_rows(size, dt):
 def test_bias_gradients_of_few_and_many_rows(size, dt):
     check_bwd(dt, *size, "gelu")
     check_bwd(dt, *size, "none", accumulate=True)
+
+
+@pytest.mark.parametrize("din", [2304, 2305])
+def test_tensors_beyond_32_bit_offsets(din):
+    """x and dx of 4.8 GB (2^31 elements lie within them), whole rows and rows that are copied."""
+    rows, dout = (1 << 20) + 3, 40
+    g = torch.Generator(device="cuda").manual_seed(35)
+    x = torch.empty(rows, din, dtype=torch.bfloat16, device="cuda")
+    for c in x.split(1 << 17):
+        c.copy_(torch.randn(c.shape, generator=g, device="cuda"))
+    w = rnd(torch.Generator().manual_seed(36), dout, din, dtype=torch.bfloat16)
+    y = singa.linear_fwd(x, w)
+    dx, dw, db = singa.linear_bwd(x, w, y)
+    u = u_of(torch.bfloat16)
+    half = (1 << 31) // din
+    for a in (0, half - 2, (1 << 30) // din - 2, rows - 5):
+        xs, ys = x[a:a + 5].double(), y[a:a + 5].double()
+        off = G(din) * (xs.abs() @ w.double().abs().t())
+        ref = xs @ w.double().t()
+        within("y", y[a:a + 5], ref, off + u * (ref.abs() + off))
+        off = G(dout) * (ys.abs() @ w.double().abs())
+        ref = ys @ w.double()
+        within("dx", dx[a:a + 5], ref, off + u * (ref.abs() + off))
+    ref, mag = torch.zeros(dout, din, dtype=torch.double, device="cuda"), torch.zeros(dout, din, dtype=torch.double, device="cuda")
+    for xs, ys in zip(x.split(1 << 16), y.split(1 << 16)):
+        ref += ys.double().t() @ xs.double()
+        mag += ys.double().abs().t() @ xs.double().abs()
+    within("dw", dw, ref, G(rows) * mag)
+    within("db", db, y.double().sum(0), G(rows) * y.double().abs().sum(0))
+    labels = torch.randint(0, dout, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    loss, dx, _, _ = singa.linear_softmax_ce(x, w, labels, need_dw=False)
+    z = x[-5:].double() @ w.double().t()
+    lse, at = torch.logsumexp(z, 1), labels[-5:].long()[:, None]
+    d = G(din) * (x[-5:].double().abs() @ w.double().abs().t()).max(1).values
+    within("rows", loss[-5:], lse - z.gather(1, at)[:, 0], 2 * d + 60 * F * (1 + 3 * lse.abs()))
+    assert bool(loss.isfinite().all()) and bool(dx[-5:].isfinite().all()) and bool((dx[-5:] != 0).any())
