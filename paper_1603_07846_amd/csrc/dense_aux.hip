@@ -228,9 +228,11 @@ __global__ __launch_bounds__(256) void dact_kernel(int act, const T* __restrict_
       float v[8], u[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = u[j] = 0.f;
-      if (row < rows) {
+      // the columns past a row's end (ldz may hold 64 more, and the last row has
+      // no next one behind it) are written as zeros and never read
+      if (row < rows && col < cols) {
         const long o = row * cols + col;
-        if (vec) {
+        if (vec) {  // a whole group of 8, or none
           load8<T>(dy + o, v);
           if (act) load8<T>(z + o, u);
         } else {
