@@ -17,8 +17,8 @@
  *     workspace, except in the pass over the weights that few rows take.
  *   - the workspace has no alignment but 16 bytes and needs no clearing; two
  *     calls whose execution may overlap need one each.
- *   - outputs may share memory with inputs or other outputs only where that is
- *     stated (UNSUPPORTED).
+ *   - outputs and the workspace may share memory with inputs, outputs or each
+ *     other only where that is stated (UNSUPPORTED).
  *   - sums are fp32 (norms fp64); bf16 outputs are rounded once, to nearest
  *     even.
  */
@@ -122,13 +122,14 @@ int singa_grad_norm(int count, const int* dtypes, const void* const* grads, cons
 /* The same, then out[i] = scale * grads[i] (rounded to the tensor's type);
  * out[i] == grads[i] clips in place, and then a scale of 1 writes nothing.
  * Outputs share memory with nothing else, so no gradient is listed twice
- * (UNSUPPORTED). */
+ * (UNSUPPORTED; singa_grad_norm, which only reads them, takes one twice). */
 int singa_grad_clip(int count, const int* dtypes, const void* const* grads, void* const* outs, const size_t* sizes,
                     float max_norm, float* stat, void* ws, size_t ws_bytes, singa_stream stream);
 
 /* singa_sgd_momentum_update and singa_adagrad_update with the gradient
  * multiplied by a factor in device memory (stat + 1 of singa_grad_norm):
- *   g' = grad_scale[0] * g + weight_decay * w, the rest as there. */
+ *   g' = grad_scale[0] * g + weight_decay * w, the rest as there.
+ * w, v (h) and w_bf16 share memory with nothing (UNSUPPORTED). */
 int singa_sgd_momentum_update_scaled(size_t n, float* w, const float* g, float* v, uint16_t* w_bf16, float lr,
                                      float momentum, float weight_decay, const float* grad_scale,
                                      singa_stream stream);

@@ -66,8 +66,8 @@ bool apart(const Span& a, const Span& b) {
   const uintptr_t pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
   return !a.p || !b.p || pa + a.bytes <= pb || pb + b.bytes <= pa;
 }
-// Workgroups write outputs while others still read: no output may share memory
-// with an input or another output.
+// Workgroups write outputs while others still read: no output, and no
+// workspace, may share memory with an input or another output.
 template <int O, int I> int check_apart(const Span (&outs)[O], const Span (&ins)[I]) {
   for (int i = 0; i < O; ++i) {
     for (int j = 0; j < i; ++j)
@@ -78,6 +78,7 @@ template <int O, int I> int check_apart(const Span (&outs)[O], const Span (&ins)
   return SINGA_OK;
 }
 Span span(const void* p, long rows, long cols, int dt) { return {p, (size_t)rows * cols * dt_size(dt)}; }
+Span ws_span(const void* ws, size_t need) { return {need ? ws : nullptr, need}; }
 
 // The row length of a matrix kept in the workspace: rows a multiple of 4 KB
 // apart would all start in the same memory channel (a product over 32768 of k:
@@ -260,9 +261,10 @@ int singa_linear_fwd(singa_dtype dtype, int rows, int in, int out, const void* x
       !aligned_to(bias, 4))
     return SINGA_ERR_ALIGN;
   FwdWs o;
-  rc = check_ws(ws, ws_bytes, carve_fwd(dtype, rows, in, out, nullptr, &o));
+  const size_t need = carve_fwd(dtype, rows, in, out, nullptr, &o);
+  rc = check_ws(ws, ws_bytes, need);
   if (rc == SINGA_OK)
-    rc = check_apart({span(y, rows, out, dtype), span(z, rows, out, dtype)},
+    rc = check_apart({span(y, rows, out, dtype), span(z, rows, out, dtype), ws_span(ws, need)},
                      {span(x, rows, in, dtype), span(w, out, in, dtype), span(bias, 1, out, F32),
                       span(residual == y ? nullptr : residual, rows, out, dtype)});
   if (rc != SINGA_OK) return rc;
@@ -332,7 +334,7 @@ int singa_linear_bwd(singa_dtype dtype, int rows, int in, int out, const void* x
     if (e == hipSuccess && db) e = launch_zero(db, (size_t)out * 4, st);
     return status(e);
   }
-  rc = check_apart({span(dx, rows, in, dtype), span(dw, out, in, dw_dtype), span(db, 1, out, F32)},
+  rc = check_apart({span(dx, rows, in, dtype), span(dw, out, in, dw_dtype), span(db, 1, out, F32), ws_span(ws, need)},
                    {span(dw ? x : nullptr, rows, in, dtype), span(dx ? w : nullptr, out, in, dtype), span(dy, rows, out, dtype),
                     span(act == SINGA_ACT_NONE ? nullptr : z, rows, out, dtype),
                     span(!dx || dx_residual == dx ? nullptr : dx_residual, rows, in, dtype)});
@@ -418,7 +420,7 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
     return status(e);
   }
   rc = check_apart({{loss, (size_t)(rows + 1L) * 4}, span(dx, rows, in, dtype), span(dw, classes, in, dw_dtype),
-                    span(db, 1, classes, F32)},
+                    span(db, 1, classes, F32), ws_span(ws, need)},
                    {span(x, rows, in, dtype), span(w, classes, in, dtype), span(bias, 1, classes, F32),
                     span(labels, rows, 1, F32)});
   if (rc != SINGA_OK) return rc;
@@ -621,7 +623,16 @@ static int grad_norm(int count, const int* dtypes, const void* const* grads, voi
     if (!aligned_to(grads[i], dt_size(dtypes[i])) || (clip && !aligned_to(outs[i], dt_size(dtypes[i])))) return SINGA_ERR_ALIGN;
   }
   if (!aligned_to(stat, 4)) return SINGA_ERR_ALIGN;
-  int rc = check_ws(ws, ws_bytes, singa_grad_norm_workspace_bytes(count));
+  const size_t need = singa_grad_norm_workspace_bytes(count);
+  int rc = check_ws(ws, ws_bytes, need);
+  // the gradients that are only read may share memory with each other
+  const Span own[] = {{stat, 2 * sizeof(float)}, ws_span(ws, need)};
+  if (rc == SINGA_OK && !apart(own[0], own[1])) rc = SINGA_ERR_UNSUPPORTED;
+  for (int i = 0; i < count && rc == SINGA_OK; ++i) {
+    const Span g{sizes[i] ? grads[i] : nullptr, sizes[i] * dt_size(dtypes[i])}, o{clip && sizes[i] ? outs[i] : nullptr, g.bytes};
+    for (const Span& w : own)
+      if (!apart(w, g) || !apart(w, o)) rc = SINGA_ERR_UNSUPPORTED;
+  }
   if (rc == SINGA_OK && clip && count) rc = clip_apart(count, dtypes, grads, outs, sizes);
   if (rc != SINGA_OK) return rc;
   return status(launch_grad_norm(count, dtypes, grads, clip ? outs : nullptr, sizes, max_norm, stat, (double*)ws,
@@ -638,12 +649,18 @@ int singa_grad_clip(int count, const int* dtypes, const void* const* grads, void
   return grad_norm(count, dtypes, grads, outs, true, sizes, max_norm, stat, ws, ws_bytes, stream);
 }
 
+// An update's own streams and the factor that every thread reads.
+static int update_apart(size_t n, const float* w, const float* g, const float* v, const uint16_t* w_bf16, const float* scale) {
+  return check_apart({Span{w, n * 4}, Span{v, n * 4}, Span{w_bf16, n * 2}}, {Span{g, n * 4}, Span{scale, 4}});
+}
+
 int singa_sgd_momentum_update_scaled(size_t n, float* w, const float* g, float* v, uint16_t* w_bf16, float lr, float momentum,
                                      float weight_decay, const float* grad_scale, singa_stream stream) {
   if (n == 0) return SINGA_OK;
   if (!w || !g || !v || !grad_scale) return SINGA_ERR_NULL;
   if (!aligned_to(w, 16) || !aligned_to(g, 16) || !aligned_to(v, 16) || !aligned_to(w_bf16, 16) || !aligned_to(grad_scale, 4))
     return SINGA_ERR_ALIGN;
+  if (update_apart(n, w, g, v, w_bf16, grad_scale) != SINGA_OK) return SINGA_ERR_UNSUPPORTED;
   return status(launch_sgd_scaled(n, w, g, v, w_bf16, lr, momentum, weight_decay, grad_scale, (hipStream_t)stream));
 }
 
@@ -653,7 +670,7 @@ int singa_adagrad_update_scaled(size_t n, float* w, const float* g, float* h, ui
   if (!w || !g || !h || !grad_scale) return SINGA_ERR_NULL;
   if (!aligned_to(w, 16) || !aligned_to(g, 16) || !aligned_to(h, 16) || !aligned_to(w_bf16, 16) || !aligned_to(grad_scale, 4))
     return SINGA_ERR_ALIGN;
-  if (!(delta > 0.f) || !(lr >= 0.f)) return SINGA_ERR_UNSUPPORTED;
+  if (!(delta > 0.f) || !(lr >= 0.f) || update_apart(n, w, g, h, w_bf16, grad_scale) != SINGA_OK) return SINGA_ERR_UNSUPPORTED;
   return status(launch_adagrad_scaled(n, w, g, h, w_bf16, lr, delta, weight_decay, grad_scale, (hipStream_t)stream));
 }
 
