@@ -16,7 +16,7 @@ enum Act { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
 //   EPI_LSE     the maximum and the sum of exponentials of v = sum + bias[col]
 //               over each STAT_COLS columns, and v at the row's label: the
 //               logits themselves are not stored
-//   EPI_DLOGITS exp(v - lse[row]) - [col is the row's label] in rows with a
+//   EPI_DLOGITS softmax(v) by lse[row] - [col is the row's label] in rows with a
 //               valid label, else 0, stored in the product's type (and, with
 //               more, what that rounding left).  The factor scale / count of the
 //               loss is left to the products that take these (alpha), so that
@@ -43,7 +43,7 @@ struct Epilogue {
   float2* stats = nullptr;  // [M][nstat] (maximum, sum), column group stat0 + ...
   int nstat = 0, stat0 = 0;
   float* zlab = nullptr;       // [M]
-  const float* lse = nullptr;  // [M]
+  const float2* lse = nullptr;  // [M], as row_lse makes them
   bf16_t* more = nullptr;  // the further terms (see TERMS), one behind the other
   int rows_padded = 0;  // dlogits rows from M up to here are zeroed (a sum over two halves reads them)
   float* colsum = nullptr;  // [row groups][N]: sums of the dlogits over COLSUM_ROWS rows
@@ -143,9 +143,9 @@ hipError_t launch_column_sums(const ColumnSums& s, hipStream_t st);
 // out (T [rows][cols]) = in (fp32 [rows][cols]), zero in rows without a valid label
 hipError_t launch_round_rows(int dt, const float* in, void* out, long rows, int cols, const int32_t* labels,
                              int classes, hipStream_t st);
-// stats [rows][nstat], zlab -> lse[row], loss[1 + row]
+// stats [rows][nstat], zlab -> lse[row] (may be null), loss[1 + row]
 hipError_t launch_lse(const float2* stats, int nstat, const float* zlab, const int32_t* labels, int classes, long rows,
-                      float* lse, float* loss, hipStream_t st);
+                      float2* lse, float* loss, hipStream_t st);
 // loss[0] = mean of loss[1 ..] over the counted rows, unit = scale / count (0 when none; may be null)
 hipError_t launch_loss_mean(const int32_t* labels, int classes, long rows, float* loss, float* unit, float scale,
                             hipStream_t st);

@@ -169,8 +169,8 @@ struct LossWs {
   int nstat, splits;  // splits, ldl: partial sums of kept logits and their row length
   long ldl;
   void *dz, *more, *xc, *xp, *wp;
-  float *unit, *lse, *zlab, *logits, *dxf, *colsum, *partial;
-  float2* stats;
+  float *unit, *zlab, *logits, *dxf, *colsum, *partial;
+  float2 *stats, *lse;
 };
 
 size_t carve_loss(int dt, int rows, int in, int classes, bool grad, int dw_dt, void* ws, LossWs* o) {
@@ -199,7 +199,7 @@ size_t carve_loss(int dt, int rows, int in, int classes, bool grad, int dw_dt, v
     o->nstat = (classes + (o->skinny ? SKINNY_COLS : STAT_COLS) - 1) / (o->skinny ? SKINNY_COLS : STAT_COLS);
     o->stats = c.take<float2>((size_t)rows * o->nstat);
     o->zlab = c.take<float>(rows);
-    o->lse = c.take<float>(rows);
+    o->lse = c.take<float2>(rows);
   }
   if (grad) {
     o->unit = c.take<float>(1);

@@ -336,7 +336,7 @@ template <int W> __device__ __forceinline__ void merge_all(float& m, float& s, f
 template <int W>
 __global__ __launch_bounds__(256) void lse_kernel(const float2* __restrict__ stats, int nstat, const float* __restrict__ zlab,
                                                   const int32_t* __restrict__ labels, int classes, long rows,
-                                                  float* __restrict__ lse, float* __restrict__ loss) {
+                                                  float2* __restrict__ lse, float* __restrict__ loss) {
   __shared__ float2 lds[4];
   const int t = threadIdx.x % W;
   const long row = workgroup() * (256 / W) + threadIdx.x / W;
@@ -346,9 +346,8 @@ __global__ __launch_bounds__(256) void lse_kernel(const float2* __restrict__ sta
   for (int i = t; i < nstat; i += W) merge(m, s, p[i].x, p[i].y);
   merge_all<W>(m, s, lds);
   if (t == 0) {
-    const float l = m + logf(s);
-    if (lse) lse[row] = l;
-    loss[1 + row] = label_ok(labels[row], classes) ? l - zlab[row] : 0.f;
+    if (lse) lse[row] = row_lse(m, s);
+    loss[1 + row] = label_ok(labels[row], classes) ? row_loss(m, s, zlab[row]) : 0.f;
   }
 }
 
@@ -414,9 +413,9 @@ __global__ __launch_bounds__(W > 256 ? W : 256) void loss_rows_kernel(LossRows a
   }
   float* zr = a.z + (size_t)(row < a.rows ? row : 0) * a.ldz;
   const size_t step = (size_t)a.rows * a.ldz;
-  float lse = 0.f;
+  float2 lse = make_float2(0.f, 0.f);
+  float m = -INFINITY, s = 0.f;
   if (live) {  // the same for all threads of a row
-    float m = -INFINITY, s = 0.f;
     constexpr int U = 4;
     for (int c0 = t; c0 < a.classes; c0 += U * W) {
       float v[U];
@@ -444,15 +443,15 @@ __global__ __launch_bounds__(W > 256 ? W : 256) void loss_rows_kernel(LossRows a
       m = mx;
     }
     merge_all<W>(m, s, lds);
-    lse = m + logf(s);
+    lse = row_lse(m, s);
   }
   if constexpr (W > 64) __syncthreads();  // the label's logit
   __builtin_amdgcn_wave_barrier();
-  if (t == 0 && row < a.rows) a.loss[1 + row] = live ? lse - zl[in_wg] : 0.f;
+  if (t == 0 && row < a.rows) a.loss[1 + row] = live ? row_loss(m, s, zl[in_wg]) : 0.f;
   if (!a.dz) return;
   for (long c = t; c < a.ldd; c += W) {
     float v = 0.f;
-    if (live && c < a.classes) v = exp_fast(zr[c] - lse) - (c == lab ? 1.f : 0.f);
+    if (live && c < a.classes) v = row_prob(zr[c], lse) - (c == lab ? 1.f : 0.f);
     store_out<T>((T*)a.dz + row * a.ldd + c, v);
     if (sizeof(T) == 2 && a.more) {
       float left = v;
@@ -519,17 +518,17 @@ __global__ __launch_bounds__(256) void loss_parts_end_kernel(LossRows a, const f
   const int lab = row < a.rows ? a.labels[row] : -1;
   const bool live = label_ok(lab, a.classes);
   float* zr = a.z + (size_t)(row < a.rows ? row : 0) * a.ldz;
-  float lse = 0.f;
+  float2 lse = make_float2(0.f, 0.f);
+  float m = -INFINITY, s = 0.f;
   if (live) {
-    float m = -INFINITY, s = 0.f;
     for (int i = threadIdx.x & 63; i < parts; i += 64) merge(m, s, stats[row * parts + i].x, stats[row * parts + i].y);
     merge_all<64>(m, s, nullptr);
-    lse = m + logf(s);
+    lse = row_lse(m, s);
   }
   const int lo = blockIdx.y * LOSS_PART, hi = (int)min((long)lo + LOSS_PART, a.dz ? a.ldd : (long)a.classes);
   // the part that holds the label, or the first one of a padding row
   if (row < a.rows && threadIdx.x == 0 && (live ? lab >= lo && lab < lo + LOSS_PART : blockIdx.y == 0))
-    a.loss[1 + row] = live ? lse - zr[lab] : 0.f;
+    a.loss[1 + row] = live ? row_loss(m, s, zr[lab]) : 0.f;
   if (!a.dz) return;
   __syncthreads();  // the label's logit is read before its place is written
   if (a.xc && row < a.rows) {
@@ -549,7 +548,7 @@ __global__ __launch_bounds__(256) void loss_parts_end_kernel(LossRows a, const f
   }
   for (int c = lo + threadIdx.x; c < hi; c += 256) {
     float v = 0.f;
-    if (live && c < a.classes) v = exp_fast(zr[c] - lse) - (c == lab ? 1.f : 0.f);
+    if (live && c < a.classes) v = row_prob(zr[c], lse) - (c == lab ? 1.f : 0.f);
     store_out<T>((T*)a.dz + row * a.ldd + c, v);
     if (sizeof(T) == 2 && a.more) {
       float left = v;
@@ -583,7 +582,7 @@ __global__ __launch_bounds__(1024) void lse_finish_kernel(const float2* __restri
     merge_all<1024>(m, s, lds);
     __syncthreads();
     const bool ok = label_ok(labels[row], classes);
-    const float l = ok ? m + logf(s) - zlab[row] : 0.f;
+    const float l = ok ? row_loss(m, s, zlab[row]) : 0.f;
     if (threadIdx.x == 0) loss[1 + row] = l;
     sum += l;
     n += ok;
@@ -608,7 +607,7 @@ __global__ __launch_bounds__(1024) void lse_finish_rows_kernel(const float2* __r
     merge_all<64>(m, s, nullptr);
     if (lane) continue;
     const bool ok = label_ok(labels[row], classes);
-    const float l = ok ? m + logf(s) - zlab[row] : 0.f;
+    const float l = ok ? row_loss(m, s, zlab[row]) : 0.f;
     loss[1 + row] = l;
     sum += l;
     n += ok;
@@ -702,7 +701,7 @@ hipError_t launch_round_rows(int dt, const float* in, void* out, long rows, int 
 }
 
 hipError_t launch_lse(const float2* stats, int nstat, const float* zlab, const int32_t* labels, int classes, long rows,
-                      float* lse, float* loss, hipStream_t st) {
+                      float2* lse, float* loss, hipStream_t st) {
   TraceScope ts("lse_kernel", st, 8.0 * rows * nstat, WORK_BYTE);
   // a wave per row, or, where rows are few, a workgroup per row
   if (rows >= 1024)

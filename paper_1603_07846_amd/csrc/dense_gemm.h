@@ -53,6 +53,17 @@ __device__ __forceinline__ v4i16 lds_tr16(const char* p) {
 // softmax lies at small |x|) besides the instruction's own ulp.
 __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 
+// A row of a softmax, from the maximum m of its logits and the sum s of their
+// exponentials relative to it.  m and the logarithm of s stay apart: their
+// rounded sum would be off by half an ulp of m, which an offset of all logits
+// makes as large as it likes (at 65536 a loss of 0.0616 came out as 0.0625).
+__device__ __forceinline__ float2 row_lse(float m, float s) { return make_float2(m, log2f(s)); }
+__device__ __forceinline__ float row_loss(float m, float s, float zlab) { return (m - zlab) + logf(s); }
+// The probability of logit z: 2^((z - m) log2(e) - log2(s)).
+__device__ __forceinline__ float row_prob(float z, float2 lse) {
+  return __builtin_amdgcn_exp2f(fmaf(z - lse.x, 1.44269504088896341f, -lse.y));
+}
+
 // erfc(x) exp(x^2) for x >= 0: t q(t) with t = 1 / (1 + 0.4375 x) and a
 // polynomial q fitted for the smallest relative error over x <= 14 (reweighted
 // least squares), 1.7e-7, 4.5e-7 as evaluated here: gelu's values far below
@@ -482,7 +493,7 @@ template <typename T, bool AKC, bool BKC, int WM, int WN, int FM, int FN> struct
   static constexpr int STAGE = TA::BYTES + TB::BYTES;
   static constexpr int PIT = FN == 4 ? 152 : FN == 2 ? 88 : 56, HALF = FN * 16 + 16;  // floats per staged row; where its odd groups start
   static_assert(PIT % 16 == 8 && PIT >= HALF + FN * 16, "rows 4 apart lie half the banks apart");
-  static constexpr int SMEM = 2 * STAGE > NW * 32 * PIT * 4 + BM * 8 ? 2 * STAGE : NW * 32 * PIT * 4 + BM * 8;
+  static constexpr int SMEM = 2 * STAGE > NW * 32 * PIT * 4 + BM * 12 ? 2 * STAGE : NW * 32 * PIT * 4 + BM * 12;
 };
 
 // A tile: WM x WN waves of (32 FM) x (32 FN).
@@ -702,17 +713,22 @@ __device__ __forceinline__ void product_tile(const GemmArgs& g, int wg, char* sm
   // is added to them a whole block ahead.
   struct RowInfo {
     int lab;
-    float lse;
+    float m, l2;  // row_lse's
   };
+  static_assert(sizeof(RowInfo) == 12, "what SMEM counts");
   RowInfo* const info = (RowInfo*)(smem + NW * 32 * PIT * 4);
   const bool rows_have = EPI != EPI_OUT || g.e.labels;
   if (rows_have) {
     for (int r = threadIdx.x; r < BM; r += NW * 64) {
       const int row = m0 + r;
-      RowInfo i{-1, 0.f};
+      RowInfo i{-1, 0.f, 0.f};
       if (row < g.M) {
         i.lab = g.e.labels[row];
-        if constexpr (EPI == EPI_DLOGITS) i.lse = g.e.lse[row];
+        if constexpr (EPI == EPI_DLOGITS) {
+          const float2 l = g.e.lse[row];
+          i.m = l.x;
+          i.l2 = l.y;
+        }
       }
       info[r] = i;
     }
@@ -899,7 +915,7 @@ __device__ __forceinline__ void product_tile(const GemmArgs& g, int wg, char* sm
 #pragma unroll
         for (int u = 0; u < UN; ++u)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) vs[u][j] = exp_fast(vs[u][j] - ris[u].lse);
+          for (int j = 0; j < 8; ++j) vs[u][j] = row_prob(vs[u][j], make_float2(ris[u].m, ris[u].l2));
         if (hit) {
 #pragma unroll
           for (int u = 0; u < UN; ++u)
