@@ -37,8 +37,8 @@ layers below; the backward loop ends by joining the two streams.
 
 With ``fused_loss`` the last fully connected layer and the softmax loss run as
 one call that does not keep the logits (singa.linear_softmax_ce): the layer
-passes its input on, and the loss layer leaves the loss and the layer's
-gradients.  With ``clip_norm`` the update is preceded by the global norm of all
+passes its input on, and the loss layer leaves the loss and, in the backward
+pass, the layer's gradients.  With ``clip_norm`` the update is preceded by the global norm of all
 gradients and takes its clipping scale from device memory.
 """
 from __future__ import annotations
@@ -283,9 +283,11 @@ class SoftmaxCELayer(Layer):
 
 
 class FusedLossLayer(Layer):
-    """The softmax loss of a fully connected layer's output without its logits;
-    the gradients of that layer come with it.  A row whose label is outside
-    [0, classes) is padding here."""
+    """The softmax loss of a fully connected layer's output without its logits.
+    The backward pass forms the gradients of that layer, and the loss with them;
+    the forward pass forms the loss alone, or, in a step whose backward pass
+    follows (deferred), nothing.  A row whose label is outside [0, classes) is
+    padding here."""
 
     def __init__(self, net, spec, fc: ConvLayer):
         self.name = spec.name
@@ -295,19 +297,24 @@ class FusedLossLayer(Layer):
         B, n = fc.in_shape[0], int(np.prod(fc.in_shape[1:]))
         self.flat = (B, n)
         self.loss = singa.empty((B + 1,), torch.float32, net.device)  # mean, then rows
-        self.workspace = singa.empty((max(256, singa.linear_softmax_ce_workspace_bytes(net.dtype, B, n, fc.K)),), torch.uint8,
-                                     net.device)
+        sizes = [singa.linear_softmax_ce_workspace_bytes(net.dtype, B, n, fc.K, grad) for grad in (False, True)]
+        self.workspace = singa.empty((max(256, *sizes),), torch.uint8, net.device)
         self.labels = None
+        self.deferred = False
         self.out_shape = (1,)
 
     def compute_feature(self, x):
-        fc, n = self.fc, self.flat[1]
-        singa.linear_softmax_ce(x.view(self.flat), fc.w_compute.view(fc.K, n), self.labels, fc.b, loss=self.loss,
-                                dx=fc.dx.view(self.flat), dw=fc.dw.view(fc.K, n), db=fc.db, workspace=self.workspace)
+        if not self.deferred:
+            fc = self.fc
+            singa.linear_softmax_ce(x.view(self.flat), fc.w_compute.view(fc.K, self.flat[1]), self.labels, fc.b, grad=False,
+                                    loss=self.loss, workspace=self.workspace)
         return self.loss
 
     def compute_gradient(self, dy=None, need_dx=True):
-        return self.fc.dx
+        fc, n = self.fc, self.flat[1]
+        singa.linear_softmax_ce(fc.x.view(self.flat), fc.w_compute.view(fc.K, n), self.labels, fc.b, loss=self.loss,
+                                dx=fc.dx.view(self.flat), dw=fc.dw.view(fc.K, n), db=fc.db, workspace=self.workspace)
+        return fc.dx
 
 
 class Net:
@@ -488,11 +495,14 @@ class Net:
         return t.to(self.device).to(self.dtype)
 
     # --------------------------------------------------------------- Alg. 1
-    def forward(self, x, labels=None):
+    def forward(self, x, labels=None, defer_loss=False):
+        """Alg. 1's forward loop.  defer_loss (train_one_batch): a fused loss is
+        left to the backward pass, which forms it with the gradients."""
         h = x
         for l in self.layers:
             if isinstance(l, (SoftmaxCELayer, FusedLossLayer)):
                 l.labels = labels
+                l.deferred = defer_loss
             h = l.compute_feature(h)
         return h
 
@@ -550,7 +560,7 @@ class Net:
                                           self.wl.momentum, self.wl.weight_decay, grad_scale=scale)
 
     def train_one_batch(self, x, labels=None, dy_top=None, need_input_grad=False):
-        self.forward(x, labels)
+        self.forward(x, labels, defer_loss=True)
         gx = self.backward(dy_top, need_input_grad, defer_join=self.wl.update)
         if self.wl.update:
             self.update()
