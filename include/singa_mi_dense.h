@@ -69,7 +69,7 @@ int singa_linear_fwd(singa_dtype dtype, int rows, int in, int out, const void* x
  * value.  rows = 0: dw and db become zero
  * (unless accumulated into).  A ReLU that passes nothing gives zero whatever
  * dy holds there.
- * Errors: as above; NULL when no output is asked for. */
+ * Errors: as above; NULL when no output is asked for (rows > 0). */
 int singa_linear_bwd_workspace_bytes(singa_dtype dtype, int rows, int in, int out, singa_act act,
                                      singa_dtype dw_dtype, size_t* bytes);
 int singa_linear_bwd(singa_dtype dtype, int rows, int in, int out, const void* x, const void* w, const void* z,

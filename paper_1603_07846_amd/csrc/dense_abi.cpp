@@ -319,7 +319,7 @@ int singa_linear_bwd(singa_dtype dtype, int rows, int in, int out, const void* x
   int rc = singa_linear_bwd_workspace_bytes(dtype, rows, in, out, act, dw_dtype, &need);
   if (rc != SINGA_OK) return rc;
   if (dw && dw_dtype == SINGA_BF16 && accumulate) return SINGA_ERR_UNSUPPORTED;
-  if (!dx && !dw && !db) return SINGA_ERR_NULL;
+  if (rows && !dx && !dw && !db) return SINGA_ERR_NULL;  // (a dx of no rows has no address)
   if (rows && (!dy || (dw && !x) || (dx && !w) || (act != SINGA_ACT_NONE && !z))) return SINGA_ERR_NULL;
   if (!aligned_to(x, 16) || !aligned_to(w, 16) || !aligned_to(z, 16) || !aligned_to(dy, 16) || !aligned_to(dx_residual, 16) ||
       !aligned_to(dx, 16) || !aligned_to(dw, 16) || !aligned_to(db, 4))
