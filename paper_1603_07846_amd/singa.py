@@ -785,16 +785,15 @@ def _grad_stat(grads, max_norm, out, stat, workspace):
         if otypes != types or osizes != sizes:
             raise ValueError("out: tensors of the gradients' sizes and types wanted")
     stat = _out("stat", stat, (2,), torch.float32, device, cur)
-    lib = _lib()  # no plan or size has loaded it yet
-    ws, at, nbytes = _dense_ws(lib.singa_grad_norm_workspace_bytes(n), device, workspace, cur)
+    ws, at, nbytes = _dense_ws(_LIB.singa_grad_norm_workspace_bytes(n), device, workspace, cur)
     # host arrays, read before the call returns
     types, sizes, ptrs, outs = array.array("i", types), array.array("Q", sizes), array.array("Q", ptrs), array.array("Q", outs)
     args = types.buffer_info()[0], ptrs.buffer_info()[0]
     rest = sizes.buffer_info()[0], max_norm, stat.data_ptr(), at, nbytes, _current_stream(cur)
     if out is None:
-        rc = lib.singa_grad_norm(n, *args, *rest)
+        rc = _LIB.singa_grad_norm(n, *args, *rest)
     else:
-        rc = lib.singa_grad_clip(n, *args, outs.buffer_info()[0], *rest)
+        rc = _LIB.singa_grad_clip(n, *args, outs.buffer_info()[0], *rest)
     if rc:
         raise SingaError("singa_grad_norm" if out is None else "singa_grad_clip", rc)
     return stat
