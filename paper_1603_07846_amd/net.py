@@ -72,9 +72,10 @@ class Layer:
 class ConvLayer(Layer):
     """Convolution (or fully connected, as a whole-input convolution)."""
 
-    def __init__(self, net, spec, in_shape, fc=False):
+    def __init__(self, net, spec, in_shape, fc=False, head=False):
         self.name = spec.name
         self.net = net
+        self.head = head  # carried out by the loss layer (Net's fused_loss): no output, no workspace, no fused update
         N, H, W, C = in_shape
         if fc:
             self.K, self.R, self.S, self.pad, self.stride = spec.out_features, H, W, 0, 1
@@ -89,18 +90,18 @@ class ConvLayer(Layer):
         self.relu = False  # set when a ReLU layer directly follows and is fused
         self.relu_src = None  # the ReLU layer feeding this one, whose backward bwd-data folds in
         self.event = None  # see _fork
-        self.head = False  # carried out by the loss layer (Net's fused_loss)
         dev, dt = net.device, net.dtype
         # update fused into the filter-gradient kernel (no workspace needed exactly then)
-        self.fused_update = bool(net.fuse_update and net.wl.update and net.updater == "sgd" and singa.conv_workspace_bytes(
-            singa.OP_BWD_FILTER_SGD, dt, self.in_shape, self.w_shape, self.pad, self.stride) == 0)
+        self.fused_update = bool(not head and net.fuse_update and net.wl.update and net.updater == "sgd"
+                                 and singa.conv_workspace_bytes(singa.OP_BWD_FILTER_SGD, dt, self.in_shape, self.w_shape,
+                                                                self.pad, self.stride) == 0)
         # update applied by the filter gradient's split-K reduction (convolutions
         # whose input the library takes as it is)
         self.reduce_update = bool(net.fuse_update and net.reduce_update and net.wl.update and net.updater == "sgd"
                                   and not self.fused_update and not fc
                                   and singa.space_to_depth_bytes(dt, self.in_shape, self.w_shape, self.pad,
                                                                  self.stride) == 0)
-        self.y = singa.empty(self.out_shape, dt, dev)
+        self.y = None if head else singa.empty(self.out_shape, dt, dev)
         self.dx = singa.empty(self.in_shape, dt, dev)
         self.x = None
         # a strided layer that the library runs on the space-to-depth form of
@@ -111,6 +112,8 @@ class ConvLayer(Layer):
             self.xs = singa.empty(singa.space_to_depth_shape(self.in_shape, self.w_shape, self.pad, self.stride),
                                   dt, dev)
         self.x_layout = "NHWC_S2D" if self.xs is not None else "NHWC"
+        if head:
+            return
         for op in (singa.OP_FWD, singa.OP_BWD_DATA, singa.OP_BWD_FILTER):
             net.need_workspace(singa.conv_workspace_bytes(op, dt, self.in_shape, self.w_shape, self.pad,
                                                           self.stride,
@@ -292,8 +295,6 @@ class FusedLossLayer(Layer):
     def __init__(self, net, spec, fc: ConvLayer):
         self.name = spec.name
         self.fc = fc
-        fc.head = True
-        fc.fused_update = fc.reduce_update = False
         B, n = fc.in_shape[0], int(np.prod(fc.in_shape[1:]))
         self.flat = (B, n)
         self.loss = singa.empty((B + 1,), torch.float32, net.device)  # mean, then rows
@@ -379,7 +380,7 @@ class Net:
             if isinstance(spec, wl.Conv):
                 layer = ConvLayer(self, spec, shape)
             elif isinstance(spec, wl.FC):
-                layer = ConvLayer(self, spec, shape, fc=True)
+                layer = ConvLayer(self, spec, shape, fc=True, head=head)
             elif isinstance(spec, wl.Pool):
                 layer = PoolLayer(self, spec, shape)
             elif isinstance(spec, wl.Relu):
