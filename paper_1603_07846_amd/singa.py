@@ -494,9 +494,22 @@ def softmax_ce(z, labels, loss=None, dz=None):
     return loss, dz
 
 
+def _update_streams(w, g, state, w_bf16):
+    """An update reads and writes w.numel() values of each: fp32, the shadow bf16, contiguous, on the current GPU."""
+    cur, n = _current(), w.numel()
+    for name, t, dtype in (("w", w, torch.float32), ("g", g, torch.float32), ("state", state, torch.float32),
+                           ("w_bf16", w_bf16, torch.bfloat16)):
+        if t is None:
+            continue
+        if t.numel() != n:
+            raise ValueError("%s: %d values wanted, got %d" % (name, n, t.numel()))
+        _dense(name, t, dtype, None, cur)
+
+
 def sgd_momentum_update(w, g, v, w_bf16=None, lr=0.01, momentum=0.9, weight_decay=0.0, grad_scale=None):
     """Fused Updater step in place on fp32 w and v (and the bf16 shadow if given).
     grad_scale: an fp32 device tensor of one value that multiplies g (grad_norm()[1:])."""
+    _update_streams(w, g, v, w_bf16)
     if grad_scale is not None:
         _check("singa_sgd_momentum_update_scaled", _lib().singa_sgd_momentum_update_scaled(
             w.numel(), _ptr(w), _ptr(g), _ptr(v), _ptr(w_bf16), float(lr), float(momentum), float(weight_decay),
@@ -534,6 +547,7 @@ def lrn_bwd(x, dy, size=5, alpha=1e-4, beta=0.75, k=1.0, layout="NHWC", out=None
 def adagrad_update(w, g, h, w_bf16=None, lr=0.01, delta=1e-6, weight_decay=0.0, grad_scale=None):
     """AdaGrad Updater step in place on fp32 w and h (and the bf16 shadow if given).
     grad_scale: as for sgd_momentum_update."""
+    _update_streams(w, g, h, w_bf16)
     if grad_scale is not None:
         _check("singa_adagrad_update_scaled", _lib().singa_adagrad_update_scaled(
             w.numel(), _ptr(w), _ptr(g), _ptr(h), _ptr(w_bf16), float(lr), float(delta), float(weight_decay),
