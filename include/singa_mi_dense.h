@@ -66,7 +66,7 @@ int singa_linear_fwd(singa_dtype dtype, int rows, int in, int out, const void* x
  *   accumulate != 0 adds into dw (fp32 only) and db.
  * bf16: the products take dz rounded to bf16; for an fp32 dw a smooth
  * activation's dz is taken in three bf16 terms, which hold all of its fp32
- * value.  rows = 0: dw and db become zero
+ * value, and cost three products (dw_dtype SINGA_BF16: one).  rows = 0: dw and db become zero
  * (unless accumulated into).  A ReLU that passes nothing gives zero whatever
  * dy holds there.
  * Errors: as above; NULL when no output is asked for (rows > 0). */
@@ -95,8 +95,13 @@ int singa_linear_bwd(singa_dtype dtype, int rows, int in, int out, const void* x
  * each row's maximum and sum, then pieces of the classes are formed again,
  * as gradients, for the products with w and x.  Logits of at most 64 MiB are
  * kept in the workspace instead of being formed twice.  The reported
- * workspace holds pieces of 256 MiB (three times that where dw is fp32 and the
- * tensors bf16), the copies that odd row lengths need, and x.
+ * workspace holds the gradients at the logits of a piece of the classes, at most
+ * 256 MiB (or 256 classes; all of rows x classes where they fit), three times
+ * that where dw is fp32 and the tensors bf16, the copies that odd row lengths
+ * need, and x.
+ * An offset that all logits of a row share costs the loss and the gradients no
+ * precision beyond the logits' own.  bf16: dx and a bf16 dw take dz rounded to
+ * bf16, an fp32 dw in three terms, as above.
  * Errors: as above. */
 int singa_linear_softmax_ce_workspace_bytes(singa_dtype dtype, int rows, int in, int classes, int gradients,
                                             singa_dtype dw_dtype, size_t* bytes);
@@ -109,9 +114,11 @@ int singa_linear_softmax_ce(singa_dtype dtype, int rows, int in, int classes, co
  * pointers, sizes and types; read before the call returns):
  *   stat[0] = norm = sqrt(sum over tensors and elements of g^2)
  *   stat[1] = scale = norm > max_norm ? max_norm / norm : 1
- * A norm that is infinite or NaN leaves scale at 1: stat[0] tells.  max_norm
- * >= 0 (infinity: the norm alone).  Squares are summed in fp64, in a fixed
- * order, so no gradient that fp32 holds overflows or vanishes in them.
+ * A gradient that is infinite or NaN makes the norm so and leaves scale at 1:
+ * stat[0] tells.  max_norm >= 0 (infinity: the norm alone).  Squares are summed
+ * in fp64, in a fixed order, so no gradient that fp32 holds overflows or
+ * vanishes in them; a norm beyond fp32 is reported as infinity in stat[0], while
+ * scale is still max_norm over its fp64 value.
  *   stat : fp32 [2] (written);  ws : singa_grad_norm_workspace_bytes()
  * Errors: NULL (also a tensor's pointer), SHAPE (count < 0), UNSUPPORTED
  * (a type, max_norm), ALIGN, WORKSPACE, HIP. */

@@ -159,8 +159,25 @@ size_t carve_bwd(int dt, int rows, int in, int out, int act, int dw_dt, void* ws
 }
 
 // ------------------------------------------------------------------- loss
-constexpr size_t kKeep = 64u << 20;    // logits of up to this many bytes are kept
-constexpr size_t kPiece = 256u << 20;  // dlogits of a piece of the classes
+// Logits of up to kKeep bytes (fp32) are kept between the two passes, larger
+// ones are formed twice, kPiece bytes of dlogits (a term) at a time.  Kept /
+// formed twice, us for loss and gradients of 1024 inputs, rows x classes:
+//   fp32  256 x 1000 51 / 123, 256 x 16000 253 / 310, 512 x 32000 872 / 1032,
+//         1024 x 32000 1739 / 2010, 4096 x 32000 6684 / 7885: keeping is faster
+//         throughout, and the limit is what the workspace may cost
+//   bf16  256 x 1000 30 / 46, 256 x 4000 47 / 60, 256 x 8000 (8 MB) 72 / 74, 512 x
+//         16000 169 / 157, 512 x 32000 299 / 258, 1024 x 32000 650 / 464, 4096 x
+//         32000 2074 / 1569, with 4096 inputs 2048 x 32000 2628 / 2663: the
+//         product is cheap beside the traffic of fp32 logits, and from 8 MB up
+//         to the limit keeping costs up to 16 %, with few inputs more (128
+//         inputs, 512 x 32000 175 / 92; 256, 2000 x 4000 102 / 79)
+// The loss alone: bf16 256 x 1000 16 / 16, with 4096 inputs 21 / 37; 512 x 16000 44
+// / 28; fp32 512 x 16000 148 / 133, 256 x 4000 34 / 75.
+// Pieces of 128 / 256 / 1024 MiB, bf16: 4096 x 2048 x 100000 8781 / 8733 / 8950
+// us, 2048 x 1024 x 200000 5551 / 5065 / 5053, 8192 x 1024 x 50000 5199 / 4944 /
+// 5556; fp32 4096 x 512 x 100000 12840 / 12538 / 13073.
+constexpr size_t kKeep = 64u << 20;
+constexpr size_t kPiece = 256u << 20;
 
 struct LossWs {
   Packed k;
@@ -193,7 +210,10 @@ size_t carve_loss(int dt, int rows, int in, int classes, bool grad, int dw_dt, v
   if (o->keep) {
     o->splits = o->skinny ? 1 : product_splits(dt, rows, classes, in);
     o->logits = c.take<float>((size_t)o->splits * rows * o->ldl);
-    // rows that do not fill the chip, and several parts of each
+    // rows that do not fill the chip, and several parts of each (in two launches:
+    // 64 x 50000 bf16 86 us against 107 with a workgroup per row, fp32 137
+    // against 155; at 10000 classes 43 against 40, and from 256 rows on 60
+    // against 53, 500 x 30000 177 against 172)
     o->stats = rows < 512 && classes > 2 * LOSS_PART ? c.take<float2>((size_t)rows * loss_parts(classes)) : nullptr;
   } else {
     o->nstat = (classes + (o->skinny ? SKINNY_COLS : STAT_COLS) - 1) / (o->skinny ? SKINNY_COLS : STAT_COLS);

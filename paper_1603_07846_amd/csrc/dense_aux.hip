@@ -206,7 +206,8 @@ __global__ __launch_bounds__(256) void zero_kernel(uint16_t* p, size_t n) {
 }
 
 // A workgroup: `rpw` rows of 256 columns, a thread 8 columns of every eighth row.
-// Bound by memory (4000 x 4096 bf16: 4.0 TB/s), few rows by the latency of a
+// Bound by memory (4000 x 4096 bf16, GELU, 98 MB: 21 us, 4.6 TB/s; with the two
+// further terms, 164 MB, 31 us, 5.3), few rows by the latency of a
 // thread's rows one after the other, so that a workgroup takes fewer of them.
 template <typename T>
 __global__ __launch_bounds__(256) void dact_kernel(int act, const T* __restrict__ dy, const T* __restrict__ z,
@@ -703,7 +704,9 @@ hipError_t launch_round_rows(int dt, const float* in, void* out, long rows, int 
 hipError_t launch_lse(const float2* stats, int nstat, const float* zlab, const int32_t* labels, int classes, long rows,
                       float2* lse, float* loss, hipStream_t st) {
   TraceScope ts("lse_kernel", st, 8.0 * rows * nstat, WORK_BYTE);
-  // a wave per row, or, where rows are few, a workgroup per row
+  // a wave per row, or, where rows are few, a workgroup per row (loss alone, bf16,
+  // 64 inputs, wave / workgroup: 300 x 100000 45 / 39 us, 600 x 100000 63 / 57,
+  // 900 x 32000 41 / 39, 1500 x 100000 126 / 120, 3000 x 32000 101 / 102)
   if (rows >= 1024)
     hipLaunchKernelGGL(lse_kernel<64>, grid_of((rows + 3) / 4), dim3(256), 0, st, stats, nstat, zlab, labels, classes,
                        rows, lse, loss);

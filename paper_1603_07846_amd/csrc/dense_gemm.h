@@ -49,8 +49,10 @@ __device__ __forceinline__ v4i16 lds_tr16(const char* p) {
 }
 
 // exp in the hardware's base-2 form: x log2(e) is rounded once, so the result
-// is off by at most |x| 2^-24 relative (x <= 0 here, and what matters of a
-// softmax lies at small |x|) besides the instruction's own ulp.
+// is off by at most |x| 2^-24 relative besides the instruction's own ulp.  A
+// softmax's x is not above 0, and what matters of it lies at small |x|; the
+// activations in bf16, where x may be up to 88 before it overflows to the right
+// limit, lose 2^-17 of a value that is rounded to 2^-8.
 __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 
 // A row of a softmax, from the maximum m of its logits and the sum s of their
@@ -1061,7 +1063,9 @@ template <typename T> __global__ __launch_bounds__(256) void product_reduce_kern
 //   128: bf16 0.44 while there is one workgroup per CU and 1.0 at two, fp32
 //        1.95 times the workgroups per CU; 5 per tile
 //   64:  0.55 times the workgroups per CU; 4 per tile
-// and a cut costs the second launch, 4, and its partial sums' bytes at 6 TB/s.
+// and a cut costs the second launch, 4, and its partial sums' bytes at 6 TB/s
+// (also where the sums are left raw and their reader adds them up: product_splits
+// takes the same plan).
 enum { TILE_128 = 0, TILE_256 = 1, TILE_64 = 2 };
 struct Plan {
   int tile, splits, kt_split;

@@ -815,8 +815,8 @@ def _grad_stat(grads, max_norm, out, stat, workspace):
 
 def grad_norm(grads, max_norm=float("inf"), stat=None, workspace=None):
     """The global norm over all gradient tensors (fp32 and bf16, mixed) and the factor that clips it to max_norm: an
-    fp32 device tensor (norm, scale), scale = max_norm / norm where norm > max_norm and is finite, else 1.  The
-    updates take stat[1:] as grad_scale."""
+    fp32 device tensor (norm, scale), scale = max_norm / norm where norm > max_norm and is finite (in fp64, in which
+    it is formed), else 1.  The updates take stat[1:] as grad_scale."""
     return _grad_stat(list(grads), max_norm, None, stat, workspace)
 
 
