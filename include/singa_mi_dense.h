@@ -66,9 +66,9 @@ int singa_linear_fwd(singa_dtype dtype, int rows, int in, int out, const void* x
  *   accumulate != 0 adds into dw (fp32 only) and db.
  * bf16: the products take dz rounded to bf16; for an fp32 dw a smooth
  * activation's dz is taken in three bf16 terms, which hold all of its fp32
- * value, and cost three products (dw_dtype SINGA_BF16: one).  rows = 0: dw and db become zero
- * (unless accumulated into).  A ReLU that passes nothing gives zero whatever
- * dy holds there.
+ * value, and cost three products (dw_dtype SINGA_BF16: one).  rows = 0: dw and
+ * db become zero (unless accumulated into).  A ReLU that passes nothing gives
+ * zero whatever dy holds there.
  * Errors: as above; NULL when no output is asked for (rows > 0). */
 int singa_linear_bwd_workspace_bytes(singa_dtype dtype, int rows, int in, int out, singa_act act,
                                      singa_dtype dw_dtype, size_t* bytes);

@@ -69,3 +69,20 @@ def test_only_the_backward_pass_forms_gradients():
     singa.trace_enable(False)
     # a whole step forms the logits once
     assert sum(n in ("skinny_kernel", "product_kernel<logits>", "product_kernel<lse>") for n in names) == 1
+
+
+def test_evaluations_between_replays():
+    net, x, labels = build(BF16, 24, fused_loss=True, clip_norm=1e-2)
+    ref, _, _ = build(BF16, 24, fused_loss=True, clip_norm=1e-2)
+    torch.cuda.synchronize()
+    graph = net.capture(x, labels)
+    other = torch.flip(x, (0,)).contiguous()
+    for i in range(4):
+        graph.replay()
+        loss = net.layers[-1].loss.clone()
+        ref.train_one_batch(x, labels)
+        assert torch.equal(net.w_flat, ref.w_flat) and torch.equal(loss, ref.layers[-1].loss), i
+        grads = net.g_flat.clone()
+        net.forward(other, labels)
+        torch.cuda.synchronize()
+        assert torch.equal(net.g_flat, grads) and not torch.equal(net.layers[-1].loss, loss)
